@@ -69,7 +69,8 @@ typedef enum {
     PROM_ERR_WORKSPACE,    /* workspace too small */
     PROM_ERR_UNSUPPORTED,  /* the requested variant cannot run this shape */
     PROM_ERR_CUDA,         /* a CUDA runtime/driver call failed */
-    PROM_ERR_TIMEOUT       /* a bounded device-side wait ran out */
+    PROM_ERR_TIMEOUT,      /* a bounded device-side wait ran out */
+    PROM_ERR_RANGE         /* a number or a type outside the documented range, an index outside its table */
 } prom_status;
 
 typedef enum {
@@ -233,6 +234,64 @@ prom_status prom_pw_conv_i8_dyn(const int8_t *x_dev, int batch, int64_t rows_per
  * PROM_ERR_TIMEOUT in prom_last_device_status.  batch == 0 is a no-op. */
 prom_status prom_quantize_act_absmax(const float *x_dev, int batch, int64_t per_sample,
                                      int8_t *q_dev, float *gamma_dev, float *scale_dev,
+                                     void *cuda_stream);
+
+/* The types of the calls below that take or give floating values. */
+typedef enum {
+    PROM_TYPE_F32 = 0,
+    PROM_TYPE_BF16,
+    PROM_TYPE_F16
+} prom_type;
+
+/* Layer norm over the rows of x[m][n] (the step in front of a projection in a transformer; the paper's networks
+ * normalise over the batch instead):
+ *     mean = sum x / n,  rstd = 1 / sqrt(sum (x - mean)^2 / n + eps),  y = (x - mean) * rstd * weight + bias
+ * Sums and products in binary32, y rounded once to its type.
+ *   x_dev, y_dev      values of `type`, row r at r * x_pitch and r * y_pitch values (pitches of n at least); y_dev may
+ *                     be x_dev itself with the same pitch and must not overlap it in any other way
+ *   weight_dev, bias_dev   [n] of `param_type`, either may be NULL (1 and 0)
+ *   mean_dev, rstd_dev     [m] float32 for the backward pass, either may be NULL
+ * 0 <= m < 2^31, 1 <= n <= 65536, eps finite and not negative.  Any pointer that is aligned to its type is taken;
+ * bases of 16 bytes, with pitches and n of whole 16-byte pieces, run fastest.  A row with a value that is not finite
+ * gives what the formula gives.  Asynchronous on the stream.
+ * Errors: PROM_ERR_NULL, PROM_ERR_SHAPE, PROM_ERR_ALIGN, PROM_ERR_RANGE (a type, eps), PROM_ERR_CUDA; m == 0 is a no-op. */
+prom_status prom_layer_norm(const void *x_dev, prom_type type, int64_t m, int n, int64_t x_pitch,
+                            const void *weight_dev, const void *bias_dev, prom_type param_type, double eps,
+                            void *y_dev, int64_t y_pitch, float *mean_dev, float *rstd_dev, void *cuda_stream);
+
+/* Layer norm and activation quantiser in one pass: y as above, never written, quantised per row as
+ * prom_quantize_act_absmax does with a sample per row,
+ *     gamma = max |y|,  scale = 127 / max(gamma, 1e-5),  q = clip(round(y * scale), -128, 127)     ties to even
+ * so that q and gamma are what a projection takes (rows_per_sample 1).  Mean and variance are taken in binary64, mean
+ * and rstd rounded once to binary32, and x - mean, * rstd, * weight, + bias, the quotient and the last product are
+ * single binary32 operations in this order: the codes do not depend on how the work is split.
+ *   q_dev  [m][n] int8;  gamma_dev, scale_dev  [m] float32;  mean_dev, rstd_dev  [m] float32 or NULL (for
+ *          prom_layer_norm_backward behind a quantiser that passes gradients straight through)
+ * A row with a value that is not finite has a gamma that is not finite and codes without meaning.  Everything else as
+ * in prom_layer_norm. */
+prom_status prom_layer_norm_i8(const void *x_dev, prom_type type, int64_t m, int n, int64_t x_pitch,
+                               const void *weight_dev, const void *bias_dev, prom_type param_type, double eps,
+                               int8_t *q_dev, float *gamma_dev, float *scale_dev, float *mean_dev, float *rstd_dev,
+                               void *cuda_stream);
+
+/* Backward pass of prom_layer_norm.  With g = dy * weight and xh = (x - mean) * rstd,
+ *     dx = rstd * (g - sum(g) / n - xh * sum(g * xh) / n),   dweight = sum_r dy * xh,   dbias = sum_r dy
+ * in binary32, each result rounded once.  The sums over the rows are added in a fixed order: the same call on the same
+ * device gives the same bits.
+ *   dy_dev, x_dev, dx_dev   values of `type` with their pitches; dx_dev may be dy_dev or x_dev with the same pitch, or
+ *                           NULL (not wanted)
+ *   weight_dev              [n] of param_type, or NULL (1)
+ *   mean_dev, rstd_dev      [m] float32, as the forward pass gave them
+ *   dweight_dev, dbias_dev  [n] of param_type, overwritten; either may be NULL.  With m == 0 they are set to zero
+ *   workspace_dev           16-byte aligned, prom_layer_norm_backward_workspace_bytes(m, n) bytes
+ *                           (PROM_ERR_WORKSPACE if smaller); not read when dweight_dev and dbias_dev are NULL
+ * Two launches.  Limits and errors as for prom_layer_norm; a copy that does not land within 0.1 s sets PROM_ERR_TIMEOUT
+ * in prom_last_device_status. */
+size_t prom_layer_norm_backward_workspace_bytes(int64_t m, int n);
+prom_status prom_layer_norm_backward(const void *dy_dev, const void *x_dev, prom_type type, int64_t m, int n,
+                                     int64_t dy_pitch, int64_t x_pitch, const void *weight_dev, prom_type param_type,
+                                     const float *mean_dev, const float *rstd_dev, void *dx_dev, int64_t dx_pitch,
+                                     void *dweight_dev, void *dbias_dev, void *workspace_dev, size_t workspace_bytes,
                                      void *cuda_stream);
 
 /* Host helper: the fixed-point pair for a real per-channel scale (alpha_i times

@@ -21,7 +21,7 @@ NATIVE_PATH = os.path.join(_HERE, "_native.so")
 
 PROM_OK = 0
 (PROM_ERR_NULL, PROM_ERR_SHAPE, PROM_ERR_ALIGN, PROM_ERR_BAD_WEIGHT, PROM_ERR_BAD_REQUANT,
- PROM_ERR_WORKSPACE, PROM_ERR_UNSUPPORTED, PROM_ERR_CUDA, PROM_ERR_TIMEOUT) = range(1, 10)
+ PROM_ERR_WORKSPACE, PROM_ERR_UNSUPPORTED, PROM_ERR_CUDA, PROM_ERR_TIMEOUT, PROM_ERR_RANGE) = range(1, 11)
 
 VARIANTS = {"auto": 0, "tc": 1, "smallk": 2, "addsub": 3, "naive": 4}
 
@@ -37,6 +37,7 @@ EXPORTS = [
     "prom_pw_prepared_bytes", "prom_pw_prepare", "prom_pw_conv_i8_prepared", "prom_quantize_ternary_batch",
     "prom_debug_dw_variant", "prom_debug_tc_wide", "prom_debug_mma_issue_rate", "prom_debug_l2_copy_rate",
     "prom_debug_mma_beside",
+    "prom_layer_norm", "prom_layer_norm_i8", "prom_layer_norm_backward", "prom_layer_norm_backward_workspace_bytes",
 ]
 STATIC_SCRATCH_BYTES = 6 << 20
 
@@ -152,6 +153,15 @@ def lib():
         L.prom_quantize_ternary_batch.argtypes = [C.POINTER(PromQuantizeJob), i32, vp]
         L.prom_quantize_ternary.restype = i32
         L.prom_quantize_ternary.argtypes = [vp, i32, i32, vp, sz, vp, vp]
+        dbl = C.c_double
+        L.prom_layer_norm.restype = i32
+        L.prom_layer_norm.argtypes = [vp, i32, i64, i32, i64, vp, vp, i32, dbl, vp, i64, vp, vp, vp]
+        L.prom_layer_norm_i8.restype = i32
+        L.prom_layer_norm_i8.argtypes = [vp, i32, i64, i32, i64, vp, vp, i32, dbl, vp, vp, vp, vp, vp, vp]
+        L.prom_layer_norm_backward_workspace_bytes.restype = sz
+        L.prom_layer_norm_backward_workspace_bytes.argtypes = [i64, i32]
+        L.prom_layer_norm_backward.restype = i32
+        L.prom_layer_norm_backward.argtypes = [vp, vp, i32, i64, i32, i64, i64, vp, i32, vp, vp, vp, i64, vp, vp, vp, sz, vp]
         L.prom_requant_from_scale.restype = i32
         L.prom_requant_from_scale.argtypes = [C.c_double, C.POINTER(C.c_int32), C.POINTER(C.c_int8)]
         L.prom_last_device_status.restype = i32
@@ -262,6 +272,66 @@ def quantize_act_absmax(x: torch.Tensor, out=None, stream=None):
         q, gamma, scale = out
     _check((_native or native()).quantize_act_absmax(x, q, gamma, scale, _handle(stream)), "prom_quantize_act_absmax")
     return q, gamma, scale
+
+
+def _empty(shape, dtype, device, stream):
+    """An uninitialised tensor that belongs to the stream which the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+               eps: float = 1e-5, out=None, stream=None):
+    """prom_layer_norm: x [..., n] float32, bfloat16 or float16 on the device (a matrix may have any row pitch)
+    -> (y like x, mean, rstd float32, one value a row); `out` may carry the three tensors, y being x itself or the
+    last two None."""
+    if out is None:
+        m = x.numel() // max(1, x.shape[-1])
+        out = (_empty(x.shape, x.dtype, x.device, stream), _empty((m,), torch.float32, x.device, stream),
+               _empty((m,), torch.float32, x.device, stream))
+    y, mean, rstd = out
+    _check((_native or native()).layer_norm(x, weight, bias, eps, y, mean, rstd, _handle(stream)), "prom_layer_norm")
+    return y, mean, rstd
+
+
+def layer_norm_i8(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                  eps: float = 1e-5, out=None, stats=None, stream=None):
+    """prom_layer_norm_i8: x as in layer_norm -> (q int8 like x, gamma, scale float32, one value a row); `out` may
+    carry the three tensors, `stats` a pair (mean, rstd) of float32 tensors to be written too."""
+    if out is None:
+        m = x.numel() // max(1, x.shape[-1])
+        out = (_empty(x.shape, torch.int8, x.device, stream), _empty((m,), torch.float32, x.device, stream),
+               _empty((m,), torch.float32, x.device, stream))
+    q, gamma, scale = out
+    mean, rstd = stats or (None, None)
+    _check((_native or native()).layer_norm_i8(x, weight, bias, eps, q, gamma, scale, mean, rstd, _handle(stream)),
+           "prom_layer_norm_i8")
+    return q, gamma, scale
+
+
+def layer_norm_backward_workspace_bytes(m: int, n: int) -> int:
+    return int(lib().prom_layer_norm_backward_workspace_bytes(m, n))
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], mean: torch.Tensor,
+                        rstd: torch.Tensor, out=None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """prom_layer_norm_backward: dy and x [..., n], the forward pass's mean and rstd -> (dx like x, dweight, dbias
+    [n] of weight's type, float32 without a weight); `out` may carry the three tensors, None for one that is not
+    wanted, dx being dy or x itself."""
+    n = x.shape[-1]
+    if out is None:
+        kept = torch.float32 if weight is None else weight.dtype
+        out = (_empty(x.shape, x.dtype, x.device, stream), _empty((n,), kept, x.device, stream),
+               _empty((n,), kept, x.device, stream))
+    dx, dweight, dbias = out
+    if workspace is None and (dweight is not None or dbias is not None):
+        nbytes = layer_norm_backward_workspace_bytes(x.numel() // max(1, n), n)
+        workspace = _empty((nbytes,), torch.uint8, x.device, stream)
+    _check((_native or native()).layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace,
+                                                     _handle(stream)), "prom_layer_norm_backward")
+    return dx, dweight, dbias
 
 
 def debug_tc_plan(fold: int = 0, nt: int = 0, groups: int = 0, occ: int = 0, stages: int = 0) -> None:

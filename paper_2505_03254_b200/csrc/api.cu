@@ -31,6 +31,7 @@
 #include "block.cuh"
 #include "stack.cuh"
 #include "quantize.cuh"
+#include "layernorm.cuh"
 #include "peak.cuh"
 
 namespace prom {
@@ -2200,6 +2201,159 @@ __global__ void dyn_clear_kernel(float *__restrict__ gamma_y, int batch)
 
 }  // namespace prom
 
+// ---- layer norm ------------------------------------------------------------------------------------
+namespace prom { namespace norm {
+
+static inline bool type_ok(int t) { return t == PROM_TYPE_F32 || t == PROM_TYPE_BF16 || t == PROM_TYPE_F16; }
+static inline size_t type_bytes(int t) { return t == PROM_TYPE_F32 ? 4 : 2; }
+static inline bool aligned_to(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+constexpr int kMaxN = 65536;
+
+static prom_status check_rows(int type, int64_t m, int n, int64_t pitch, const void *p)
+{
+    if (pitch < n || pitch > (1ll << 40)) return PROM_ERR_SHAPE;
+    if (m > 0 && !p) return PROM_ERR_NULL;
+    return aligned_to(p, type_bytes(type)) ? PROM_OK : PROM_ERR_ALIGN;
+}
+static prom_status check_vector(int type, const void *p)
+{
+    return aligned_to(p, type_bytes(type)) ? PROM_OK : PROM_ERR_ALIGN;
+}
+static prom_status check_common(int type, int param_type, int64_t m, int n)
+{
+    if (!type_ok(type) || !type_ok(param_type)) return PROM_ERR_RANGE;
+    return m < 0 || m >= (1ll << 31) || n < 1 || n > kMaxN ? PROM_ERR_SHAPE : PROM_OK;
+}
+// Rows made of whole 16-byte pieces.
+static bool whole_pieces(const void *p, int64_t pitch, size_t bytes) { return aligned16(p) && (size_t)pitch * bytes % 16 == 0; }
+
+template <class K, class P>
+static prom_status launch(K *kernel, const P &p, long long grid, int threads, size_t smem, cudaStream_t st)
+{
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[1];
+    fill_launch_cfg(cfg, attr, (int)grid, threads, smem, st, true);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, p);
+    ++g_launches;
+    return cuda_status(e);
+}
+
+// V accesses a thread: a warp per row up to 128 accesses, else the block that they fill.
+template <class T, int E, int V, bool CODES>
+static prom_status launch_forward(const Fwd &p, cudaStream_t st)
+{
+    const int pieces = p.n / E;
+    if (pieces <= 32 * V)
+        return launch(forward_kernel<T, E, V, CODES, true>, p, (p.m + 7) / 8, 256, 0, st);
+    return launch(forward_kernel<T, E, V, CODES, false>, p, p.m, (pieces + 32 * V - 1) / (32 * V) * 32, 0, st);
+}
+
+template <class T, bool CODES>
+static prom_status run_forward(const Fwd &p, bool wide, cudaStream_t st)
+{
+    if (wide) {
+        const int pieces = p.n / kWide<T>;
+        if (pieces <= 32) return launch_forward<T, kWide<T>, 1, CODES>(p, st);
+        if (pieces <= 64 || (pieces > 128 && pieces <= 2048)) return launch_forward<T, kWide<T>, 2, CODES>(p, st);
+        if (pieces <= 4096) return launch_forward<T, kWide<T>, 4, CODES>(p, st);
+    } else {
+        if (p.n <= 128 || (p.n > 512 && p.n <= 4096)) return launch_forward<T, 1, 4, CODES>(p, st);
+        if (p.n <= 16384) return launch_forward<T, 1, 16, CODES>(p, st);
+    }
+    return launch(forward_long_kernel<T, CODES>, p, p.m, 1024, 0, st);
+}
+
+static prom_status forward(const void *x, int type, int64_t m, int n, int64_t x_pitch, const void *w, const void *b, int ptype,
+                           double eps, void *y, int64_t y_pitch, int8_t *q, float *gamma, float *scale, float *mean,
+                           float *rstd, cudaStream_t st)
+{
+    prom_status s = check_common(type, ptype, m, n);
+    if (s != PROM_OK) return s;
+    if (!(eps >= 0.0) || !(eps <= 3.0e38)) return PROM_ERR_RANGE;
+    if ((s = check_rows(type, m, n, x_pitch, x)) != PROM_OK) return s;
+    if (q || gamma || scale) {
+        if (m > 0 && (!q || !gamma || !scale)) return PROM_ERR_NULL;
+        if (!aligned_to(gamma, 4) || !aligned_to(scale, 4)) return PROM_ERR_ALIGN;
+    } else if ((s = check_rows(type, m, n, y_pitch, y)) != PROM_OK) {
+        return s;
+    }
+    if ((s = check_vector(ptype, w)) != PROM_OK || (s = check_vector(ptype, b)) != PROM_OK) return s;
+    if (!aligned_to(mean, 4) || !aligned_to(rstd, 4)) return PROM_ERR_ALIGN;
+    if (m == 0) return PROM_OK;
+    if (!q && y == x && x_pitch != y_pitch && m > 1) return PROM_ERR_SHAPE;
+    const size_t bytes = type_bytes(type);
+    const bool wide = whole_pieces(x, x_pitch, bytes) && (q ? aligned_to(q, 8) : whole_pieces(y, y_pitch, bytes)) &&
+                      (size_t)n * bytes % 16 == 0 && aligned16(w) && aligned16(b);
+    const Fwd p{x, m, x_pitch, y_pitch, n, {w, ptype}, {b, ptype}, eps, y, q, mean, rstd, gamma, scale};
+    if (type == PROM_TYPE_F32) return q ? run_forward<float, true>(p, wide, st) : run_forward<float, false>(p, wide, st);
+    if (type == PROM_TYPE_BF16)
+        return q ? run_forward<__nv_bfloat16, true>(p, wide, st) : run_forward<__nv_bfloat16, false>(p, wide, st);
+    return q ? run_forward<__half, true>(p, wide, st) : run_forward<__half, false>(p, wide, st);
+}
+
+template <class T, int E, int V, bool RING>
+static prom_status launch_backward(Bwd &p, const DeviceInfo &d, int &blocks, cudaStream_t st)
+{
+    const int pieces = p.n / E;
+    p.group = (pieces + 32 * V - 1) / (32 * V) * 32;
+    p.groups = kBwdThreads<E, V> / p.group;
+    // few rows: spread over the SMs before they share one
+    const long long each = (p.m + d.sms - 1) / d.sms;
+    if (each < p.groups) p.groups = (int)each;
+    const long long want = (p.m + p.groups - 1) / p.groups;
+    blocks = (int)(want < d.sms ? want : d.sms);
+    p.stages = 0;
+    size_t smem = p.part ? (size_t)2 * p.n_pad * 4 : 0;
+    if (RING) {
+        // rows in flight: as many as fit, up to eight a group
+        const size_t stage = (size_t)2 * p.n * sizeof(T) * p.groups;
+        const size_t room = (size_t)d.smem_optin - 4096;
+        p.stages = (int)(room / stage < (size_t)kMaxStages ? room / stage : (size_t)kMaxStages);
+        if (p.stages > p.group) p.stages = p.group;
+        const size_t bytes = stage * p.stages;
+        if (bytes > smem) smem = bytes;
+    }
+    if (raise_smem_limit(backward_kernel<T, E, V, RING>, d.smem_optin - 4096) != cudaSuccess) return PROM_ERR_CUDA;
+    return launch(backward_kernel<T, E, V, RING>, p, blocks, p.group * p.groups, smem, st);
+}
+
+template <class T>
+static prom_status run_backward(Bwd &p, bool wide, const DeviceInfo &d, int &blocks, cudaStream_t st)
+{
+    if (wide) {
+        constexpr int E = kWide<T>;
+        const int pieces = p.n / E;
+        if (pieces <= 32) return launch_backward<T, E, 1, true>(p, d, blocks, st);
+        if (pieces <= 64 * (kBwdThreads<E, 2> / 32)) return launch_backward<T, E, 2, true>(p, d, blocks, st);
+        if (pieces <= 128 * (kBwdThreads<E, 4> / 32)) return launch_backward<T, E, 4, true>(p, d, blocks, st);
+    } else {
+        if (p.n <= 4 * kBwdThreads<1, 4>) return launch_backward<T, 1, 4, false>(p, d, blocks, st);
+        if (p.n <= 16 * kBwdThreads<1, 16>) return launch_backward<T, 1, 16, false>(p, d, blocks, st);
+    }
+    // the column sums first: dx may be dy or x
+    if (p.part) {
+        blocks = (int)(p.m < d.sms ? p.m : d.sms);
+        const long long each = (p.m + blocks - 1) / blocks;
+        blocks = (int)((p.m + each - 1) / each);
+        cudaLaunchConfig_t cfg;
+        cudaLaunchAttribute attr[1];
+        fill_launch_cfg(cfg, attr, 1, 256, 0, st, true);
+        cfg.gridDim = dim3((unsigned)((p.n_pad + 255) / 256), (unsigned)blocks);
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, column_sums_kernel<T>, p, each);
+        ++g_launches;
+        if (e != cudaSuccess) return cuda_status(e);
+    }
+    return p.dx ? launch(backward_long_kernel<T>, p, p.m, 1024, 0, st) : PROM_OK;
+}
+
+static size_t backward_workspace(int64_t m, int n, int sms)
+{
+    return (size_t)(m < sms ? m : sms) * 2 * (size_t)((n + 3) & ~3) * sizeof(float);
+}
+
+}}  // namespace prom::norm
+
 using namespace prom;
 
 extern "C" {
@@ -2487,6 +2641,85 @@ prom_status prom_quantize_act_absmax(const float *x_dev, int batch, int64_t per_
                                                             scale_dev);
     ++g_launches;
     return cuda_status(cudaGetLastError());
+}
+
+prom_status prom_layer_norm(const void *x_dev, prom_type type, int64_t m, int n, int64_t x_pitch, const void *weight_dev,
+                            const void *bias_dev, prom_type param_type, double eps, void *y_dev, int64_t y_pitch,
+                            float *mean_dev, float *rstd_dev, void *cuda_stream)
+{
+    return norm::forward(x_dev, (int)type, m, n, x_pitch, weight_dev, bias_dev, (int)param_type, eps, y_dev, y_pitch, nullptr,
+                         nullptr, nullptr, mean_dev, rstd_dev, static_cast<cudaStream_t>(cuda_stream));
+}
+
+prom_status prom_layer_norm_i8(const void *x_dev, prom_type type, int64_t m, int n, int64_t x_pitch, const void *weight_dev,
+                               const void *bias_dev, prom_type param_type, double eps, int8_t *q_dev, float *gamma_dev,
+                               float *scale_dev, float *mean_dev, float *rstd_dev, void *cuda_stream)
+{
+    if (m > 0 && (!q_dev || !gamma_dev || !scale_dev)) return PROM_ERR_NULL;
+    return norm::forward(x_dev, (int)type, m, n, x_pitch, weight_dev, bias_dev, (int)param_type, eps, nullptr, n, q_dev,
+                         gamma_dev, scale_dev, mean_dev, rstd_dev, static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t prom_layer_norm_backward_workspace_bytes(int64_t m, int n)
+{
+    if (m < 1 || m >= (1ll << 31) || n < 1 || n > norm::kMaxN) return 0;
+    const DeviceInfo d = device_info();
+    return d.ok ? norm::backward_workspace(m, n, d.sms) : 0;
+}
+
+prom_status prom_layer_norm_backward(const void *dy_dev, const void *x_dev, prom_type type, int64_t m, int n, int64_t dy_pitch,
+                                     int64_t x_pitch, const void *weight_dev, prom_type param_type, const float *mean_dev,
+                                     const float *rstd_dev, void *dx_dev, int64_t dx_pitch, void *dweight_dev,
+                                     void *dbias_dev, void *workspace_dev, size_t workspace_bytes, void *cuda_stream)
+{
+    prom_status s = norm::check_common((int)type, (int)param_type, m, n);
+    if (s != PROM_OK) return s;
+    if ((s = norm::check_rows((int)type, m, n, dy_pitch, dy_dev)) != PROM_OK) return s;
+    if ((s = norm::check_rows((int)type, m, n, x_pitch, x_dev)) != PROM_OK) return s;
+    if (dx_dev && (s = norm::check_rows((int)type, m, n, dx_pitch, dx_dev)) != PROM_OK) return s;
+    if (m > 0 && (!mean_dev || !rstd_dev)) return PROM_ERR_NULL;
+    const int pt = (int)param_type;
+    if (!norm::aligned_to(mean_dev, 4) || !norm::aligned_to(rstd_dev, 4) || norm::check_vector(pt, weight_dev) != PROM_OK ||
+        norm::check_vector(pt, dweight_dev) != PROM_OK || norm::check_vector(pt, dbias_dev) != PROM_OK)
+        return PROM_ERR_ALIGN;
+    if (m > 1 && ((dx_dev == dy_dev && dx_dev && dx_pitch != dy_pitch) || (dx_dev == x_dev && dx_dev && dx_pitch != x_pitch)))
+        return PROM_ERR_SHAPE;
+    const bool sums = dweight_dev || dbias_dev;
+    if (!sums && (!dx_dev || m == 0)) return PROM_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (sums && m > 0 && (!workspace_dev || !aligned16(workspace_dev))) return workspace_dev ? PROM_ERR_ALIGN : PROM_ERR_NULL;
+    DeviceInfo d = device_info();
+    if (!d.ok) return PROM_ERR_CUDA;
+    if (sums && m > 0 && workspace_bytes < norm::backward_workspace(m, n, d.sms)) return PROM_ERR_WORKSPACE;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[1];
+    if (m == 0) {
+        fill_launch_cfg(cfg, attr, (n + 255) / 256, 256, 0, st, true);
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, norm::zero_kernel, n, dweight_dev, dbias_dev, pt);
+        ++g_launches;
+        return cuda_status(e);
+    }
+    norm::Bwd p;
+    memset(&p, 0, sizeof(p));
+    p.dy = dy_dev; p.x = x_dev; p.m = m; p.dy_pitch = dy_pitch; p.x_pitch = x_pitch; p.dx_pitch = dx_pitch; p.n = n;
+    p.w.p = weight_dev; p.w.type = pt;
+    p.mean = mean_dev; p.rstd = rstd_dev; p.dx = dx_dev;
+    p.part = sums ? static_cast<float *>(workspace_dev) : nullptr;
+    p.n_pad = (n + 3) & ~3;
+    const size_t bytes = norm::type_bytes((int)type);
+    const bool wide = norm::whole_pieces(x_dev, x_pitch, bytes) && norm::whole_pieces(dy_dev, dy_pitch, bytes) &&
+                      (!dx_dev || norm::whole_pieces(dx_dev, dx_pitch, bytes)) && (size_t)n * bytes % 16 == 0 &&
+                      aligned16(weight_dev);
+    int blocks = 0;
+    if (type == PROM_TYPE_F32) s = norm::run_backward<float>(p, wide, d, blocks, st);
+    else if (type == PROM_TYPE_BF16) s = norm::run_backward<__nv_bfloat16>(p, wide, d, blocks, st);
+    else s = norm::run_backward<__half>(p, wide, d, blocks, st);
+    if (s != PROM_OK || !sums) return s;
+    fill_launch_cfg(cfg, attr, (2 * p.n_pad + 127) / 128, 256, 0, st, true);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, norm::backward_sum_kernel, (const float *)p.part, blocks, n, p.n_pad, dweight_dev,
+                                             dbias_dev, pt);
+    ++g_launches;
+    return cuda_status(e);
 }
 
 prom_status prom_requant_from_scale(double scale, int32_t *mult, int8_t *shift)
@@ -2991,6 +3224,7 @@ const char *prom_status_string(prom_status s)
     case PROM_ERR_UNSUPPORTED: return "variant does not support this shape";
     case PROM_ERR_CUDA: return "CUDA call failed";
     case PROM_ERR_TIMEOUT: return "device-side wait ran out";
+    case PROM_ERR_RANGE: return "number, type or index out of range";
     default: return "unknown status";
     }
 }

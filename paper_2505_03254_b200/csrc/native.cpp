@@ -38,6 +38,8 @@ const char *dtype_name(at::ScalarType t)
     case at::kChar: return "torch.int8";
     case at::kByte: return "torch.uint8";
     case at::kInt: return "torch.int32";
+    case at::kBFloat16: return "torch.bfloat16";
+    case at::kHalf: return "torch.float16";
     default: return "torch.float32";
     }
 }
@@ -296,6 +298,149 @@ PyObject *pw_layer_seq(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- float matrices: their type, their rows and how far these are apart --------------------------------------
+prom_type float_type(const at::Tensor &t, const char *name)
+{
+    switch (t.scalar_type()) {
+    case at::kFloat: return PROM_TYPE_F32;
+    case at::kBFloat16: return PROM_TYPE_BF16;
+    case at::kHalf: return PROM_TYPE_F16;
+    default: fail(PyExc_ValueError, "%s must be float32, bfloat16 or float16", name);
+    }
+}
+
+// The library launches on the current device: a tensor elsewhere would be another device's pointer there.
+void here(const at::Tensor &t, const char *name)
+{
+    if (!t.is_cuda()) fail(PyExc_ValueError, "%s must be a CUDA tensor", name);
+    if (t.device().index() != c10::cuda::current_device()) fail(PyExc_ValueError, "%s must be on the current CUDA device", name);
+}
+
+struct Rows {
+    void *p;
+    prom_type type;
+    int64_t m, pitch;
+    int n;
+};
+
+// [..., n] with dense rows: any pitch between the rows of a matrix, none between those of more dimensions.
+Rows rows(PyObject *o, const char *name)
+{
+    const at::Tensor &t = tensor(o, name);
+    here(t, name);
+    if (t.dim() < 1) fail(PyExc_ValueError, "%s must have a dimension at least", name);
+    const int64_t n = t.size(-1);
+    if (n > INT32_MAX) fail(PyExc_ValueError, "%s has too many columns", name);
+    if (t.dim() == 2 ? n > 1 && t.stride(1) != 1 : !t.is_contiguous()) fail(PyExc_ValueError, "%s must have dense rows", name);
+    int64_t m = 1;
+    for (int64_t i = 0; i + 1 < t.dim(); ++i) m *= t.size(i);
+    return {t.data_ptr(), float_type(t, name), m, t.dim() == 2 && m > 1 ? t.stride(0) : n, (int)n};
+}
+
+void same(const Rows &a, const Rows &b, const char *name)
+{
+    if (a.m != b.m || a.n != b.n || a.type != b.type) fail(PyExc_ValueError, "%s must have x's shape and type", name);
+}
+
+// A dense vector of `n` values of type `t`; None gives no pointer.
+void *vector(PyObject *o, int64_t n, at::ScalarType t, const char *name)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &v = dev(o, t, name);
+    here(v, name);
+    if (v.numel() != n) fail(PyExc_ValueError, "%s has another number of values than the rows need", name);
+    return v.data_ptr();
+}
+
+// The parameters of a norm have one type: the first one's that is there.
+at::ScalarType param_type(PyObject *a, PyObject *b, PyObject *c, prom_type &type)
+{
+    for (PyObject *o : {a, b, c})
+        if (o != Py_None) {
+            const at::Tensor &t = tensor(o, "a parameter");
+            type = float_type(t, "a parameter");
+            return t.scalar_type();
+        }
+    type = PROM_TYPE_F32;
+    return at::kFloat;
+}
+
+double real(PyObject *o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw ArgError();
+    return v;
+}
+
+// (x, weight, bias, eps, y, mean, rstd, stream)
+PyObject *layer_norm(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 8, [&] {
+        const Rows x = rows(a[0], "x"), y = rows(a[4], "y");
+        same(x, y, "y");
+        prom_type pt;
+        const at::ScalarType pts = param_type(a[1], a[2], Py_None, pt);
+        const void *w = vector(a[1], x.n, pts, "weight"), *b = vector(a[2], x.n, pts, "bias");
+        const double eps = real(a[3]);
+        auto *mean = static_cast<float *>(vector(a[5], x.m, at::kFloat, "mean"));
+        auto *rstd = static_cast<float *>(vector(a[6], x.m, at::kFloat, "rstd"));
+        void *st = stream(a[7]);
+        return call([&] { return prom_layer_norm(x.p, x.type, x.m, x.n, x.pitch, w, b, pt, eps, y.p, y.pitch, mean, rstd, st); });
+    });
+}
+
+// (x, weight, bias, eps, q, gamma, scale, mean, rstd, stream)
+PyObject *layer_norm_i8(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 10, [&] {
+        const Rows x = rows(a[0], "x");
+        prom_type pt;
+        const at::ScalarType pts = param_type(a[1], a[2], Py_None, pt);
+        const void *w = vector(a[1], x.n, pts, "weight"), *b = vector(a[2], x.n, pts, "bias");
+        const double eps = real(a[3]);
+        auto *q = static_cast<int8_t *>(vector(a[4], x.m * x.n, at::kChar, "q"));
+        auto *gamma = static_cast<float *>(vector(a[5], x.m, at::kFloat, "gamma"));
+        auto *scale = static_cast<float *>(vector(a[6], x.m, at::kFloat, "scale"));
+        auto *mean = static_cast<float *>(vector(a[7], x.m, at::kFloat, "mean"));
+        auto *rstd = static_cast<float *>(vector(a[8], x.m, at::kFloat, "rstd"));
+        void *st = stream(a[9]);
+        return call([&] { return prom_layer_norm_i8(x.p, x.type, x.m, x.n, x.pitch, w, b, pt, eps, q, gamma, scale, mean, rstd, st); });
+    });
+}
+
+// (dy, x, weight, mean, rstd, dx, dweight, dbias, workspace, stream)
+PyObject *layer_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 10, [&] {
+        const Rows x = rows(a[1], "x"), dy = rows(a[0], "dy");
+        same(x, dy, "dy");
+        Rows dx{nullptr, x.type, x.m, x.n, x.n};
+        if (a[5] != Py_None) {
+            dx = rows(a[5], "dx");
+            same(x, dx, "dx");
+        }
+        prom_type pt;
+        const at::ScalarType pts = param_type(a[2], a[6], a[7], pt);
+        const void *w = vector(a[2], x.n, pts, "weight");
+        const auto *mean = static_cast<const float *>(vector(a[3], x.m, at::kFloat, "mean"));
+        const auto *rstd = static_cast<const float *>(vector(a[4], x.m, at::kFloat, "rstd"));
+        void *dw = vector(a[6], x.n, pts, "dweight"), *db = vector(a[7], x.n, pts, "dbias");
+        void *ws = nullptr;
+        size_t ws_bytes = 0;
+        if (a[8] != Py_None) {
+            const at::Tensor &t = dev(a[8], at::kByte, "workspace");
+            here(t, "workspace");
+            ws = t.data_ptr();
+            ws_bytes = (size_t)t.numel();
+        }
+        void *st = stream(a[9]);
+        return call([&] {
+            return prom_layer_norm_backward(dy.p, x.p, x.type, x.m, x.n, dy.pitch, x.pitch, w, pt, mean, rstd, dx.p, dx.pitch,
+                                            dw, db, ws, ws_bytes, st);
+        });
+    });
+}
+
 // (prom_requant, prom_layer, prom_quantize_job as the binding has them); kept for as long as the module
 PyObject *register_types(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -312,7 +457,8 @@ PyObject *register_types(PyObject *, PyObject *const *a, Py_ssize_t n)
 #define ENTRY(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(pw_conv_i8), ENTRY(pw_conv_i8_res), ENTRY(pw_conv_i8_prepared), ENTRY(pw_conv_i8_dyn),
                          ENTRY(dw_conv3x3_i8), ENTRY(quantize_act_absmax), ENTRY(quantize_ternary_batch),
-                         ENTRY(pw_layer_seq), ENTRY(register_types), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(pw_layer_seq), ENTRY(layer_norm), ENTRY(layer_norm_i8), ENTRY(layer_norm_backward),
+                         ENTRY(register_types), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -294,6 +294,46 @@ prom_status prom_layer_norm_backward(const void *dy_dev, const void *x_dev, prom
                                      void *dweight_dev, void *dbias_dev, void *workspace_dev, size_t workspace_bytes,
                                      void *cuda_stream);
 
+/* Low-rank adapters: n pairs of thin matrices A[rank][cin] and B[cout][rank], dense, of one 16-bit type. */
+typedef struct {
+    const void *a_dev;          /* [n][rank][cin], 16-byte aligned */
+    const void *b_dev;          /* [n][cout][rank], 16-byte aligned */
+    const float *scale_dev;     /* [n], or NULL: 1 for every adapter */
+    prom_type type;             /* PROM_TYPE_BF16 or PROM_TYPE_F16 */
+    int n, rank;                /* 0 <= n <= 2^20, 1 <= rank <= 256 */
+} prom_adapters;
+
+/* A ternary projection with float outputs and the low-rank adapters of many requests beside it.  The packed weights are
+ * frozen and shared (Figure 12, inference branch: the integer convolution first, the scales applied to its result); a
+ * request that was fine-tuned brings an adapter.  With s = r / rows_per_sample the sample of row r,
+ * f = max(gamma_x[s], 1e-5) / 127 and a = adapter_of_sample[s],
+ *     y[r][o] = (sum_k x[r][k] * W-hat[o][k]) * alpha[o] * f
+ *             + scale[a] * f * sum_j B[a][o][j] * (sum_k A[a][j][k] * x[r][k])          (a >= 0)
+ * The first sum is exact, the others and the factors are taken in binary32 (the inner products, where the tensor cores
+ * take them as 16-bit values, as a sum of two such values, or of three for float32 outputs), y is rounded once.
+ *   x_dev        [batch * rows_per_sample][cin] int8, 16-byte aligned; gamma_x_dev [batch] float32 (both as
+ *                prom_layer_norm_i8 and prom_quantize_act_absmax give them: one sample a token, or an image)
+ *   w_packed_dev, alpha_dev   as for prom_pw_conv_i8_dyn
+ *   adapters     NULL or n == 0: the projection alone
+ *   adapter_of_sample_dev     [batch] int32: 0 .. n - 1, or -1 for no adapter.  Any order, any number of samples may share
+ *                one.  Another value counts as -1 and sets PROM_ERR_RANGE in the device status word
+ *   y_dev        [batch * rows_per_sample] rows of cout values of y_type, y_pitch >= cout values apart; must overlap no
+ *                input.  What lies between the rows is not written
+ *   workspace_dev             16-byte aligned, prom_pw_proj_adapters_workspace_bytes(batch, rows_per_sample, rank) bytes,
+ *                not read without adapters.  Calls that may overlap need workspaces of their own
+ * cin a multiple of 16, cout a multiple of 8, both up to 4096 (PROM_ERR_UNSUPPORTED, PROM_ERR_SHAPE).  The values of an
+ * adapter should be finite: a value of B that is not counts as zero and sets PROM_ERR_BAD_WEIGHT in the device status
+ * word, one of A shows in the rows of its own samples only.  Weight codes that are not valid surface as
+ * PROM_ERR_BAD_WEIGHT.  Asynchronous on the stream (at most two launches); batch == 0 is a no-op.
+ * Errors: PROM_ERR_NULL, PROM_ERR_SHAPE, PROM_ERR_ALIGN, PROM_ERR_RANGE (a type), PROM_ERR_WORKSPACE,
+ * PROM_ERR_UNSUPPORTED, PROM_ERR_CUDA; a wait that runs out sets PROM_ERR_TIMEOUT in prom_last_device_status. */
+size_t prom_pw_proj_adapters_workspace_bytes(int batch, int64_t rows_per_sample, int rank);
+prom_status prom_pw_proj_adapters(const int8_t *x_dev, int batch, int64_t rows_per_sample, int cin,
+                                  const uint8_t *w_packed_dev, int cout, const float *alpha_dev, const float *gamma_x_dev,
+                                  const prom_adapters *adapters, const int32_t *adapter_of_sample_dev, void *y_dev,
+                                  prom_type y_type, int64_t y_pitch, void *workspace_dev, size_t workspace_bytes,
+                                  void *cuda_stream);
+
 /* Host helper: the fixed-point pair for a real per-channel scale (alpha_i times
  * the activation scales and whatever BatchNorm folds in; Figure 12 divides by
  * these in floating point): mult in [2^30, 2^31) and shift in [0, 31] with

@@ -38,6 +38,7 @@ EXPORTS = [
     "prom_debug_dw_variant", "prom_debug_tc_wide", "prom_debug_mma_issue_rate", "prom_debug_l2_copy_rate",
     "prom_debug_mma_beside",
     "prom_layer_norm", "prom_layer_norm_i8", "prom_layer_norm_backward", "prom_layer_norm_backward_workspace_bytes",
+    "prom_pw_proj_adapters", "prom_pw_proj_adapters_workspace_bytes",
 ]
 STATIC_SCRATCH_BYTES = 6 << 20
 
@@ -56,6 +57,11 @@ class PromLayer(C.Structure):
 class PromQuantizeJob(C.Structure):
     _fields_ = [("w_dev", C.c_void_p), ("cout", C.c_int), ("cin", C.c_int), ("packed_dev", C.c_void_p),
                 ("packed_bytes", C.c_size_t), ("alpha_dev", C.c_void_p)]
+
+
+class PromAdapters(C.Structure):
+    _fields_ = [("a_dev", C.c_void_p), ("b_dev", C.c_void_p), ("scale_dev", C.c_void_p), ("type", C.c_int),
+                ("n", C.c_int), ("rank", C.c_int)]
 
 
 class PromError(RuntimeError):
@@ -162,6 +168,11 @@ def lib():
         L.prom_layer_norm_backward_workspace_bytes.argtypes = [i64, i32]
         L.prom_layer_norm_backward.restype = i32
         L.prom_layer_norm_backward.argtypes = [vp, vp, i32, i64, i32, i64, i64, vp, i32, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+        L.prom_pw_proj_adapters_workspace_bytes.restype = sz
+        L.prom_pw_proj_adapters_workspace_bytes.argtypes = [i32, i64, i32]
+        L.prom_pw_proj_adapters.restype = i32
+        L.prom_pw_proj_adapters.argtypes = [vp, i32, i64, i32, vp, i32, vp, vp, C.POINTER(PromAdapters), vp, vp, i32, i64,
+                                            vp, sz, vp]
         L.prom_requant_from_scale.restype = i32
         L.prom_requant_from_scale.argtypes = [C.c_double, C.POINTER(C.c_int32), C.POINTER(C.c_int8)]
         L.prom_last_device_status.restype = i32
@@ -332,6 +343,29 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
     _check((_native or native()).layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace,
                                                      _handle(stream)), "prom_layer_norm_backward")
     return dx, dweight, dbias
+
+
+def pw_proj_adapters_workspace_bytes(batch: int, rows_per_sample: int, rank: int) -> int:
+    return int(lib().prom_pw_proj_adapters_workspace_bytes(batch, rows_per_sample, rank))
+
+
+def pw_proj_adapters(x: torch.Tensor, batch: int, w_packed: torch.Tensor, cout: int, alpha: torch.Tensor,
+                     gamma_x: torch.Tensor, a: Optional[torch.Tensor] = None, b: Optional[torch.Tensor] = None,
+                     scale: Optional[torch.Tensor] = None, adapter_of_sample: Optional[torch.Tensor] = None,
+                     y: Optional[torch.Tensor] = None, dtype=torch.bfloat16, workspace: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
+    """prom_pw_proj_adapters: x int8 [batch * rows_per_sample, cin], alpha float32 [cout], gamma_x float32 [batch],
+    adapters a [n, rank, cin] and b [n, cout, rank] (bfloat16 or float16), scale float32 [n] or None, adapter_of_sample
+    int32 [batch] (-1: none), all on the device -> y [batch * rows_per_sample, cout].  `y` may be given, a matrix of any
+    row pitch and of any of the three float types; otherwise it is made in `dtype`."""
+    if y is None:
+        y = _empty((x.shape[0], cout), dtype, x.device, stream)
+    if workspace is None and a is not None and a.shape[0] and batch:
+        nbytes = pw_proj_adapters_workspace_bytes(batch, x.shape[0] // batch, a.shape[1])
+        workspace = _empty((nbytes,), torch.uint8, x.device, stream)
+    _check((_native or native()).pw_proj_adapters(x, batch, w_packed, cout, alpha, gamma_x, a, b, scale, adapter_of_sample,
+                                                  y, workspace, _handle(stream)), "prom_pw_proj_adapters")
+    return y
 
 
 def debug_tc_plan(fold: int = 0, nt: int = 0, groups: int = 0, occ: int = 0, stages: int = 0) -> None:

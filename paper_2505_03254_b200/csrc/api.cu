@@ -32,6 +32,7 @@
 #include "stack.cuh"
 #include "quantize.cuh"
 #include "layernorm.cuh"
+#include "adapters.cuh"
 #include "peak.cuh"
 
 namespace prom {
@@ -2354,6 +2355,52 @@ static size_t backward_workspace(int64_t m, int n, int sms)
 
 }}  // namespace prom::norm
 
+// ---- the projection with adapters -------------------------------------------------------------------
+namespace prom { namespace lora {
+
+constexpr int kMaxRank = 256;
+
+template <class H, class Y, int MO, int MT>
+static prom_status launch_rows(const Params &p, cudaStream_t st)
+{
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[1];
+    fill_launch_cfg(cfg, attr, 1, 32 * kRowWarps, 0, st, true);
+    cfg.gridDim = dim3((unsigned)((p.cout + 16 * MO - 1) / (16 * MO)), (unsigned)((p.m + 8 * MT - 1) / (8 * MT)));
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, proj_rows_kernel<H, Y, MO, MT>, p);
+    ++g_launches;
+    return cuda_status(e);
+}
+
+template <class H, class Y>
+static prom_status run_rows(Params &p, cudaStream_t st)
+{
+    if (p.a) {
+        cudaLaunchConfig_t cfg;
+        cudaLaunchAttribute attr[1];
+        fill_launch_cfg(cfg, attr, 1, 256, 0, st, true);
+        cfg.gridDim = dim3((unsigned)p.m, (unsigned)((p.rank + 7) / 8));
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, inner_rows_kernel<H>, p);
+        ++g_launches;
+        if (e != cudaSuccess) return cuda_status(e);
+        p.chained = 1;
+    }
+    if (p.m <= 8) return launch_rows<H, Y, 1, 1>(p, st);
+    return launch_rows<H, Y, 2, 4>(p, st);
+}
+
+template <class H>
+static prom_status run(Params &p, int y_type, cudaStream_t st)
+{
+    if (y_type == PROM_TYPE_F32) return run_rows<H, float>(p, st);
+    if (y_type == PROM_TYPE_BF16) return run_rows<H, __nv_bfloat16>(p, st);
+    return run_rows<H, __half>(p, st);
+}
+
+static size_t workspace_bytes(long long m, int rank) { return round256((size_t)m * rank * sizeof(float)); }
+
+}}  // namespace prom::lora
+
 using namespace prom;
 
 extern "C" {
@@ -2720,6 +2767,55 @@ prom_status prom_layer_norm_backward(const void *dy_dev, const void *x_dev, prom
                                              dbias_dev, pt);
     ++g_launches;
     return cuda_status(e);
+}
+
+size_t prom_pw_proj_adapters_workspace_bytes(int batch, int64_t rows_per_sample, int rank)
+{
+    if (batch < 1 || rows_per_sample < 1 || rank < 1 || rank > lora::kMaxRank || rows_per_sample >= (1ll << 31) ||
+        batch * rows_per_sample >= (1ll << 31))
+        return 0;
+    return lora::workspace_bytes(batch * rows_per_sample, rank);
+}
+
+prom_status prom_pw_proj_adapters(const int8_t *x_dev, int batch, int64_t rows_per_sample, int cin,
+                                  const uint8_t *w_packed_dev, int cout, const float *alpha_dev, const float *gamma_x_dev,
+                                  const prom_adapters *adapters, const int32_t *adapter_of_sample_dev, void *y_dev,
+                                  prom_type y_type, int64_t y_pitch, void *workspace_dev, size_t workspace_bytes,
+                                  void *cuda_stream)
+{
+    if (batch < 0 || rows_per_sample < 1 || cin < 1 || cout < 1 || cin > 4096 || cout > 4096) return PROM_ERR_SHAPE;
+    if (rows_per_sample >= (1ll << 31) || batch * rows_per_sample >= (1ll << 31)) return PROM_ERR_SHAPE;
+    if (y_pitch < cout || y_pitch > (1ll << 40)) return PROM_ERR_SHAPE;
+    if (!norm::type_ok((int)y_type)) return PROM_ERR_RANGE;
+    const bool with = adapters && adapters->n != 0;
+    if (with) {
+        if (adapters->type != PROM_TYPE_BF16 && adapters->type != PROM_TYPE_F16) return PROM_ERR_RANGE;
+        if (adapters->n < 0 || adapters->n > (1 << 20) || adapters->rank < 1 || adapters->rank > lora::kMaxRank) return PROM_ERR_SHAPE;
+    }
+    if (cin % 16 || cout % 8) return PROM_ERR_UNSUPPORTED;
+    if (batch == 0) return PROM_OK;
+    if (!x_dev || !w_packed_dev || !alpha_dev || !gamma_x_dev || !y_dev) return PROM_ERR_NULL;
+    if (with && (!adapters->a_dev || !adapters->b_dev || !adapter_of_sample_dev || !workspace_dev)) return PROM_ERR_NULL;
+    if (!aligned16(x_dev) || !aligned16(w_packed_dev) || !norm::aligned_to(alpha_dev, 4) || !norm::aligned_to(gamma_x_dev, 4) ||
+        !norm::aligned_to(y_dev, norm::type_bytes((int)y_type)))
+        return PROM_ERR_ALIGN;
+    if (with && (!aligned16(adapters->a_dev) || !aligned16(adapters->b_dev) || !norm::aligned_to(adapters->scale_dev, 4) ||
+                 !norm::aligned_to(adapter_of_sample_dev, 4) || !aligned16(workspace_dev)))
+        return PROM_ERR_ALIGN;
+    if (static_cast<const void *>(x_dev) == y_dev) return PROM_ERR_ALIGN;
+    const long long m = batch * rows_per_sample;
+    if (with && workspace_bytes < lora::workspace_bytes(m, adapters->rank)) return PROM_ERR_WORKSPACE;
+    lora::Params p;
+    memset(&p, 0, sizeof(p));
+    p.x = x_dev; p.m = m; p.rows_per_sample = rows_per_sample; p.cin = cin; p.cout = cout; p.w = w_packed_dev;
+    p.alpha = alpha_dev; p.gamma = gamma_x_dev; p.y = y_dev; p.y_pitch = y_pitch;
+    if (with) {
+        p.a = adapters->a_dev; p.b = adapters->b_dev; p.scale = adapters->scale_dev; p.which = adapter_of_sample_dev;
+        p.n = adapters->n; p.rank = adapters->rank; p.t = static_cast<float *>(workspace_dev);
+    }
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    return with && adapters->type == PROM_TYPE_F16 ? lora::run<__half>(p, (int)y_type, st)
+                                                   : lora::run<__nv_bfloat16>(p, (int)y_type, st);
 }
 
 prom_status prom_requant_from_scale(double scale, int32_t *mult, int8_t *shift)

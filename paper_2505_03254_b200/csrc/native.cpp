@@ -441,6 +441,64 @@ PyObject *layer_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// (x, batch, w_packed, cout, alpha, gamma_x, a, b, scale, adapter_of_sample, y, workspace, stream); a None: no adapters
+PyObject *pw_proj_adapters(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 13, [&] {
+        const at::Tensor &x = dev(a[0], at::kChar, "x"), &w = dev(a[2], at::kByte, "w_packed");
+        dims(x, 2, "x");
+        here(x, "x");
+        here(w, "w_packed");
+        const int batch = small_int(a[1]), cout = small_int(a[3]);
+        const int64_t m = x.size(0), cin = x.size(1);
+        if (batch < 0 || (batch ? m % batch != 0 || m == 0 : m != 0)) fail(PyExc_ValueError, "%s must have a whole number of rows per sample", "x");
+        if (cin > INT32_MAX || cout < 0 || w.numel() != cout * ((cin + 3) / 4))
+            fail(PyExc_ValueError, "%s must have cout rows of ceil(cin / 4) bytes", "w_packed");
+        const auto *alpha = static_cast<const float *>(vector(a[4], cout, at::kFloat, "alpha"));
+        const auto *gamma = static_cast<const float *>(vector(a[5], batch, at::kFloat, "gamma_x"));
+        prom_adapters ad{nullptr, nullptr, nullptr, PROM_TYPE_BF16, 0, 1};
+        const int32_t *which = nullptr;
+        if (a[6] != Py_None) {
+            const at::Tensor &av = tensor(a[6], "a"), &bv = tensor(a[7], "b");
+            ad.type = float_type(av, "a");
+            if (ad.type == PROM_TYPE_F32) fail(PyExc_ValueError, "%s must be bfloat16 or float16", "a");
+            dev(a[6], av.scalar_type(), "a");
+            dev(a[7], av.scalar_type(), "b");
+            here(av, "a");
+            here(bv, "b");
+            dims(av, 3, "a");
+            dims(bv, 3, "b");
+            if (av.size(2) != cin) fail(PyExc_ValueError, "%s must be [adapters, rank, cin]", "a");
+            if (bv.size(0) != av.size(0) || bv.size(1) != cout || bv.size(2) != av.size(1))
+                fail(PyExc_ValueError, "%s must be [adapters, cout, rank]", "b");
+            if (av.size(0) > INT32_MAX || av.size(1) > INT32_MAX) fail(PyExc_ValueError, "%s has too many rows", "a");
+            ad.n = (int)av.size(0);
+            ad.rank = (int)av.size(1);
+            ad.a_dev = av.data_ptr();
+            ad.b_dev = bv.data_ptr();
+            ad.scale_dev = static_cast<const float *>(vector(a[8], ad.n, at::kFloat, "scale"));
+            which = static_cast<const int32_t *>(vector(a[9], batch, at::kInt, "adapter_of_sample"));
+        }
+        const Rows y = rows(a[10], "y");
+        if (y.m != m || y.n != cout) fail(PyExc_ValueError, "%s must be [rows of x, cout]", "y");
+        void *ws = nullptr;
+        size_t ws_bytes = 0;
+        if (a[11] != Py_None) {
+            const at::Tensor &t = dev(a[11], at::kByte, "workspace");
+            here(t, "workspace");
+            ws = t.data_ptr();
+            ws_bytes = (size_t)t.numel();
+        }
+        void *st = stream(a[12]);
+        const auto *xp = ptr<const int8_t>(x);
+        const auto *wp = ptr<const uint8_t>(w);
+        return call([&] {
+            return prom_pw_proj_adapters(xp, batch, batch ? m / batch : 1, (int)cin, wp, cout, alpha, gamma, &ad, which, y.p,
+                                         y.type, y.pitch, ws, ws_bytes, st);
+        });
+    });
+}
+
 // (prom_requant, prom_layer, prom_quantize_job as the binding has them); kept for as long as the module
 PyObject *register_types(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -458,6 +516,7 @@ PyObject *register_types(PyObject *, PyObject *const *a, Py_ssize_t n)
 PyMethodDef methods[] = {ENTRY(pw_conv_i8), ENTRY(pw_conv_i8_res), ENTRY(pw_conv_i8_prepared), ENTRY(pw_conv_i8_dyn),
                          ENTRY(dw_conv3x3_i8), ENTRY(quantize_act_absmax), ENTRY(quantize_ternary_batch),
                          ENTRY(pw_layer_seq), ENTRY(layer_norm), ENTRY(layer_norm_i8), ENTRY(layer_norm_backward),
+                         ENTRY(pw_proj_adapters),
                          ENTRY(register_types), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

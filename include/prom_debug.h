@@ -81,6 +81,10 @@ void prom_debug_seq_block(int mode, int rows, int split);
  * or PROM_ERR_UNSUPPORTED.  Results do not depend on it.  Process-wide. */
 void prom_debug_dw_variant(int variant);
 
+/* Which kernels prom_pw_proj_adapters runs: 0 = the library's choice by the number of rows, 1 = those for few
+ * rows (warp-level MMAs from the 2-bit codes), 2 = the tiled ones (pairs of CTAs, tensor memory).  Process-wide. */
+void prom_debug_adapters(int mode);
+
 /* Which kernel the tensor-core variant of a single pointwise call runs: 0 = the
  * library's choice (the row-resident kernel, in which a pair of CTAs keeps 256 rows with all
  * their input channels in shared memory and streams the weight matrix past them,

@@ -38,7 +38,7 @@ EXPORTS = [
     "prom_debug_dw_variant", "prom_debug_tc_wide", "prom_debug_mma_issue_rate", "prom_debug_l2_copy_rate",
     "prom_debug_mma_beside",
     "prom_layer_norm", "prom_layer_norm_i8", "prom_layer_norm_backward", "prom_layer_norm_backward_workspace_bytes",
-    "prom_pw_proj_adapters", "prom_pw_proj_adapters_workspace_bytes",
+    "prom_debug_adapters", "prom_pw_proj_adapters", "prom_pw_proj_adapters_workspace_bytes",
 ]
 STATIC_SCRATCH_BYTES = 6 << 20
 
@@ -130,6 +130,8 @@ def lib():
         L.prom_debug_tc_plan_query.argtypes = [i64, i32, i32, C.POINTER(C.c_int)]
         L.prom_debug_dw_variant.restype = None
         L.prom_debug_dw_variant.argtypes = [i32]
+        L.prom_debug_adapters.restype = None
+        L.prom_debug_adapters.argtypes = [i32]
         L.prom_debug_tc_wide.restype = None
         L.prom_debug_tc_wide.argtypes = [i32, i32]
         L.prom_debug_seq_chain.restype = None
@@ -398,6 +400,11 @@ def debug_tc_wide(mode: int = 0, blocks: int = 0) -> None:
     row-resident kernel or refuse; blocks = 128-channel blocks per column tile of that kernel (1, 2,
     0 = the planner's choice)."""
     lib().prom_debug_tc_wide(int(mode), int(blocks))
+
+
+def debug_adapters(mode: int = 0) -> None:
+    """prom_debug_adapters: 0 = the library's choice, 1 = the kernels for few rows, 2 = the tiled ones."""
+    lib().prom_debug_adapters(int(mode))
 
 
 def debug_seq_chain(mode: int = 0) -> None:

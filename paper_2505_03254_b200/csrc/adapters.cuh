@@ -9,6 +9,7 @@
 #include "common.cuh"
 #include "layernorm.cuh"
 #include "ptx.cuh"
+#include "wide.cuh"
 
 namespace prom { namespace lora {
 
@@ -24,7 +25,9 @@ struct Params {
     int n, rank;
     void *y;
     long long y_pitch;
-    float *t;                       // [m][rank] inner products (few rows)
+    float *t;                       // [m][t_pitch] inner products
+    int t_pitch;                    // rank, or rounded up to 16 with zeros behind it (many rows)
+    int *list;                      // many rows: per tile of 256 rows the number of its adapters and these
     int chained;                    // a kernel of the same call is in front: only what that one writes is waited for
 };
 
@@ -82,7 +85,7 @@ inner_rows_kernel(const Params p)
         }
     }
     sum = norm::warp_sum(sum);
-    if (lane == 0) p.t[r * p.rank + j] = sum;
+    if (lane == 0) p.t[r * p.t_pitch + j] = sum;
 }
 
 // sum_j B[a][o][j] t[j].  A value of B that is not finite counts as zero and is reported (many rows share a tile of B,
@@ -237,10 +240,607 @@ proj_rows_kernel(const Params p)
         const float f = row_factor(p, s);
         float y = (float)acc * __ldg(p.alpha + o0 + o) * f;
         const int a = adapter_of(p, s);
-        if (a >= 0) y += (p.scale ? __ldg(p.scale + a) : 1.0f) * f * outer<H>(p, a, o0 + o, p.t + r * p.rank, bad);
+        if (a >= 0) y += (p.scale ? __ldg(p.scale + a) : 1.0f) * f * outer<H>(p, a, o0 + o, p.t + r * p.t_pitch, bad);
         static_cast<Y *>(p.y)[r * p.y_pitch + o0 + o] = norm::from_float<Y>(y);
     }
     if (bad) raise_status(PROM_ERR_BAD_WEIGHT);
+}
+
+// ---- many rows: inner products ----------------------------------------------------------------------------------
+// Rows in tiles of 256.  A block sorts the tile's rows by their adapter (each thread counts the rows that come before its
+// own), so that any order of requests costs what runs of requests cost: an item is up to 64 rows of one adapter, found
+// by index.  Items go round the blocks of a tile, ranks in parts of 32 over blockIdx.z.  The eight warps share K and
+// multiply with the warp-level 16-bit MMA, rows as A (int8 values are exact in both 16-bit types) and the adapter as B; a
+// thread's 16 bytes of a row and 32 of the adapter are 16 neighbouring values of k, whose order inside the MMAs is free.
+constexpr int kTile = 256;
+constexpr int kItemRows = 64;
+constexpr int kListInts = kTile + 1;
+constexpr int kInnerWarps = 8;
+
+// Four int8 values (one word) to two words of 16-bit values: 0, 1 and 2, 3.
+template <class H> __device__ __forceinline__ void widen_4(uint32_t w, uint32_t &lo, uint32_t &hi);
+template <> __device__ __forceinline__ void widen_4<__half>(uint32_t w, uint32_t &lo, uint32_t &hi)
+{
+    // 1024 + u has u = x + 128 in its low byte
+    const uint32_t u = w ^ 0x80808080u, base = 0x64646464u;
+    const uint32_t a = __byte_perm(u, base, 0x4140), b = __byte_perm(u, base, 0x4342), off = 0x64806480u;     // 1024 + 128
+    const __half2 x = __hsub2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&off));
+    const __half2 y = __hsub2(*reinterpret_cast<const __half2 *>(&b), *reinterpret_cast<const __half2 *>(&off));
+    lo = *reinterpret_cast<const uint32_t *>(&x);
+    hi = *reinterpret_cast<const uint32_t *>(&y);
+}
+template <> __device__ __forceinline__ void widen_4<__nv_bfloat16>(uint32_t w, uint32_t &lo, uint32_t &hi)
+{
+    // 128 + (x & 127) minus 128, or minus 256 where the sign is set: all three are bfloat16 values
+    const uint32_t base = 0x43434343u;
+    const uint32_t a = __byte_perm(w, base, 0x4140), b = __byte_perm(w, base, 0x4342);
+    const uint32_t an = a & 0xFF7FFF7Fu, as = a & 0xFF80FF80u, bn = b & 0xFF7FFF7Fu, bs = b & 0xFF80FF80u;
+    const __nv_bfloat162 x = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&an), *reinterpret_cast<const __nv_bfloat162 *>(&as));
+    const __nv_bfloat162 y = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&bn), *reinterpret_cast<const __nv_bfloat162 *>(&bs));
+    lo = *reinterpret_cast<const uint32_t *>(&x);
+    hi = *reinterpret_cast<const uint32_t *>(&y);
+}
+template <class H> __device__ __forceinline__ void mma_16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <> __device__ __forceinline__ void mma_16<__nv_bfloat16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <> __device__ __forceinline__ void mma_16<__half>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Partial sums of an item: [rows][32 ranks] per warp.
+constexpr int kInnerSmem = kInnerWarps * kItemRows * 33 * (int)sizeof(float);
+
+template <class H>
+__global__ void __launch_bounds__(32 * kInnerWarps)
+inner_tiles_kernel(const Params p)
+{
+    extern __shared__ float part[];             // [warp][row][33]
+    __shared__ int key_s[kTile], row_s[kTile];  // adapters by row; rows in the order of their adapters
+    __shared__ int item_s[kTile];               // first place | rows << 16
+    __shared__ int warp_items[kTile / 32], warp_lists[kTile / 32];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const long long tile = blockIdx.x, first = tile * kTile;
+    ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
+
+    // places: rows without an adapter have none
+    const int key = first + tid < p.m ? adapter_of(p, (first + tid) / p.rows_per_sample) : -1;
+    key_s[tid] = key;
+    __syncthreads();
+    int less = 0, same_before = 0, same = 0;
+    for (int i = 0; i < kTile; ++i) {
+        const int k = key_s[i];
+        less += k >= 0 && k < key;
+        same += k == key;
+        same_before += k == key && i < tid;
+    }
+    const int place = less + same_before;
+    if (key >= 0) row_s[place] = tid;
+    // an item starts at every 64th row of an adapter; the list of adapters has their first rows
+    const bool head = key >= 0 && same_before % kItemRows == 0, newcomer = key >= 0 && same_before == 0;
+    const unsigned heads = __ballot_sync(0xFFFFFFFFu, head), news = __ballot_sync(0xFFFFFFFFu, newcomer);
+    if (lane == 0) { warp_items[warp] = __popc(heads); warp_lists[warp] = __popc(news); }
+    __syncthreads();
+    int items = 0, before = 0, adapters = 0, list_before = 0;
+    for (int w = 0; w < kTile / 32; ++w) {
+        if (w == warp) { before = items; list_before = adapters; }
+        items += warp_items[w];
+        adapters += warp_lists[w];
+    }
+    const unsigned below = (1u << lane) - 1u;
+    if (head) {
+        const int left = same - same_before;
+        item_s[before + __popc(heads & below)] = place | ((left < kItemRows ? left : kItemRows) << 16);
+    }
+    if (blockIdx.y == 0 && blockIdx.z == 0) {
+        int *list = p.list + tile * kListInts;
+        if (newcomer) list[1 + list_before + __popc(news & below)] = key;
+        if (tid == 0) list[0] = adapters;
+    }
+    __syncthreads();
+
+    const int j0 = blockIdx.z * 32, ranks = p.t_pitch - j0 < 32 ? p.t_pitch - j0 : 32;      // a multiple of 16
+    for (int it = blockIdx.y; it < items; it += gridDim.y) {
+        const int at = item_s[it] & 0xFFFF, count = item_s[it] >> 16;
+        const int a = key_s[row_s[at]];
+        const H *am = static_cast<const H *>(p.a) + (size_t)a * p.rank * p.cin;
+        float acc[4][4][4];                     // [16 rows][8 ranks][...]
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
+        const int8_t *xr[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int k = 16 * i + 8 * h + g;
+                xr[i][h] = p.x + (first + row_s[at + (k < count ? k : 0)]) * p.cin;
+            }
+        for (int k = warp * 64 + 16 * t; k < ((p.cin + 63) & ~63); k += 64 * kInnerWarps) {
+            const bool in = k < p.cin;
+            uint32_t b[4][8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int rk = j0 + 8 * j + g;
+                uint4 v0 = make_uint4(0u, 0u, 0u, 0u), v1 = v0;
+                if (8 * j < ranks && in && rk < p.rank) {
+                    const uint4 *src = reinterpret_cast<const uint4 *>(am + (size_t)rk * p.cin + k);
+                    v0 = __ldg(src); v1 = __ldg(src + 1);
+                }
+                b[j][0] = v0.x; b[j][1] = v0.y; b[j][2] = v0.z; b[j][3] = v0.w;
+                b[j][4] = v1.x; b[j][5] = v1.y; b[j][6] = v1.z; b[j][7] = v1.w;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (16 * i >= count) break;
+                uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
+                if (in) {
+                    lo = __ldg(reinterpret_cast<const uint4 *>(xr[i][0] + k));
+                    hi = __ldg(reinterpret_cast<const uint4 *>(xr[i][1] + k));
+                }
+                const uint32_t lw[4] = {lo.x, lo.y, lo.z, lo.w}, hw[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    uint32_t f[4];
+                    widen_4<H>(lw[s], f[0], f[2]);
+                    widen_4<H>(hw[s], f[1], f[3]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (8 * j < ranks) mma_16<H>(acc[i][j], f, b[j][2 * s], b[j][2 * s + 1]);
+                }
+            }
+        }
+        float *mine = part + (size_t)warp * kItemRows * 33;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (16 * i >= count) break;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mine[(16 * i + g + 8 * (e >> 1)) * 33 + 8 * j + 2 * t + (e & 1)] = acc[i][j][e];
+        }
+        __syncthreads();
+        for (int i = tid; i < count * ranks; i += 32 * kInnerWarps) {
+            const int k = i / ranks, j = i - k * ranks;
+            float s = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kInnerWarps; ++w) s += part[((size_t)w * kItemRows + k) * 33 + j];
+            p.t[(first + row_s[at + k]) * p.t_pitch + j0 + j] = s;
+        }
+        __syncthreads();
+    }
+}
+
+// ---- many rows: the projection -------------------------------------------------------------------------------------
+// Tiles of 256 rows x nt outputs by pairs of CTAs (cta_group::2, 128 rows of x and half of the tile's weights in each),
+// two accumulators in tensor memory: int32 for the projection, binary32 for the adapters, which the epilogue joins.
+// x comes by TMA.  The weights never exist as bytes in memory: eight warps expand the 2-bit codes into the swizzled
+// operand layout on their way into shared memory, so a stage takes 4 KB of weights from L2 instead of 16 (a pair's SM would
+// need 64 bytes a clock of both operands at the MMAs' rate, of the 58 that L2 gives it; this way it is 40).
+// Behind the chunks of K come those of the adapters: for each adapter of the tile the rows' inner products (zero for rows of
+// other adapters), as sums of 16-bit values (two, or three for binary32 outputs) side by side along K, against B
+// repeated as often.  A row's products are first scaled by a power of two so that they fit the 16-bit type.
+constexpr int kFillWarps = 8, kEpiWarps = 8;
+constexpr int kFill0 = 2, kEpi0 = kFill0 + kFillWarps;
+constexpr int kTileThreads = 32 * (kEpi0 + kEpiWarps);
+constexpr int kStages = 6;
+constexpr uint32_t kHalfStage = 128u * 128u, kStage = 2u * kHalfStage;      // rows of x, rows of weights: 128 bytes of K each
+constexpr uint32_t kSlab = 32u * 128u;                                      // an epilogue warp's 32 rows x 32 outputs
+constexpr uint32_t kOffSlab = kStages * kStage;
+constexpr uint32_t kOffBars = kOffSlab + kEpiWarps * kSlab;
+constexpr size_t kTileSmem = 1024 + kOffBars + 256;
+constexpr uint32_t kD2 = 256;               // column of the adapters' accumulator
+constexpr int kAhead = 4;                   // chunks of codes in registers
+
+struct Tiles {
+    Params p;
+    int kc, ksteps_last;        // chunks of 128 bytes of K; MMA steps in the last one
+    int n_mtiles, n_ctiles, nt;
+    int terms;                  // 16-bit values per inner product
+    int store;                  // y has a tensor map
+};
+
+// 16 codes to 16 bytes in order (invalid ones become -2).
+__device__ __forceinline__ uint4 expand_16(uint32_t w)
+{
+    const uint32_t even = w & 0x33333333u, odd = (w >> 2) & 0x33333333u, lut = 0xFFFE0100u;
+    const uint32_t e0 = __byte_perm(lut, 0u, even), e1 = __byte_perm(lut, 0u, even >> 16);
+    const uint32_t o0 = __byte_perm(lut, 0u, odd), o1 = __byte_perm(lut, 0u, odd >> 16);
+    return make_uint4(__byte_perm(e0, o0, 0x5140), __byte_perm(e0, o0, 0x7362), __byte_perm(e1, o1, 0x5140), __byte_perm(e1, o1, 0x7362));
+}
+
+template <class H> __device__ __forceinline__ uint32_t pack_pair(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack_pair<__nv_bfloat16>(float lo, float hi)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+template <> __device__ __forceinline__ uint32_t pack_pair<__half>(float lo, float hi)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// The power of two by which a row's inner products are divided, so that the largest lies in [2^13, 2^14): far from both ends
+// of the 16-bit types.  1 for a row of (nearly) zeros or one that has a value which is not finite.
+__device__ __forceinline__ float row_power(const float *t, int n)
+{
+    float top = 0.0f;
+    for (int j = 0; j < n; j += 4) {
+        const float4 v = *reinterpret_cast<const float4 *>(t + j);
+        top = norm::max_nan(norm::max_nan(top, fabsf(v.x)), norm::max_nan(fabsf(v.y), norm::max_nan(fabsf(v.z), fabsf(v.w))));
+    }
+    const uint32_t e = (__float_as_uint(top) >> 23) & 0xFFu;
+    return e <= 14u || e == 255u ? 1.0f : __uint_as_float((e - 13u) << 23);
+}
+
+template <class H, class Y>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
+proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap, const Tiles q)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
+    const uint32_t base = ptx::smem_u32(smem);
+    const int warp = ptx::warp_index(), lane = threadIdx.x & 31;
+    const uint32_t rank = ptx::cluster_rank();
+    const Params &p = q.p;
+
+    // In the first CTA: full (its loader's arrival, both CTAs' fillers and both loads' bytes) and tempty (both read-outs).
+    // In each: empty and tfull, by the MMAs' completion.
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + kOffBars);
+    const uint32_t bar_full = ptx::smem_u32(bars), bar_empty = bar_full + 8 * kStages;
+    const uint32_t bar_tfull = bar_empty + 8 * kStages, bar_tempty = bar_tfull + 8, bar_drain = bar_tempty + 8;
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(bars + 2 * kStages + 3);
+    volatile int *flags = reinterpret_cast<volatile int *>(bars + 2 * kStages + 4);
+
+    const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
+    const long long units = (long long)q.n_mtiles * q.n_ctiles;
+    auto width = [&](int ct) { const int left = p.cout - ct * q.nt; return left >= q.nt ? q.nt : (left + 31) & ~31; };
+    const int pitch = p.t_pitch, k2 = q.terms * pitch, per_adapter = (k2 + 63) >> 6;    // chunks of 64 values
+
+    if (warp == 0) {
+        if (lane < kStages) {
+            ptx::mbar_init(bar_full + 8 * lane, 1 + 2 * kFillWarps);
+            ptx::mbar_init(bar_empty + 8 * lane, 1);
+        } else if (lane == 31) {
+            ptx::mbar_init(bar_tfull, 1);
+            ptx::mbar_init(bar_tempty, 2 * kEpiWarps);
+            ptx::mbar_init(bar_drain, 1);
+            flags[0] = 0;
+            ptx::tma_prefetch_desc(&xmap);
+            if (q.store) ptx::tma_prefetch_desc(&ymap);
+        }
+        ptx::mbar_init_fence();
+    }
+    if (warp == 1) ptx::tmem_alloc_pair(ptx::smem_u32((const void *)tmem_slot), 512u);
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::cluster_sync();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = *tmem_slot;
+    // What a kernel in front of this call wrote: with inner_tiles_kernel in between it is complete already.
+    if (!p.chained) ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
+    auto adapters_of_tile = [&](int mt) { return p.a ? __ldcg(p.list + (size_t)mt * kListInts) : 0; };
+
+    if (warp == 0) {
+        // ---- loader of x ----------------------------------------------------------------------------------
+        const bool leader = ptx::elect_one();
+        const uint32_t full = ptx::map_to_rank(bar_full, 0);
+        uint32_t st = 0, ph = 0;
+        bool ok = true, waited = !p.chained;
+        for (long long u = pair; u < units && ok; u += pairs) {
+            const int mt = (int)(u / q.n_ctiles);
+            for (int c = 0; c < q.kc; ++c) {
+                if (!tc::wait_bar_warp(bar_empty + 8 * st, ph ^ 1u, flags)) { ok = false; break; }
+                if (leader) {
+                    if (rank == 0) ptx::mbar_expect_tx(bar_full + 8 * st, 2u * kHalfStage);
+                    ptx::tma_load_2d_pair(base + st * kStage, &xmap, c * 128, mt * kTile + (int)rank * 128, full + 8 * st);
+                }
+                if (++st == kStages) { st = 0; ph ^= 1u; }
+            }
+            if (!ok || !p.a) continue;
+            // the adapters' stages are the fillers' alone
+            if (!waited) { ptx::grid_dep_wait(); waited = true; }
+            const uint32_t skip = (uint32_t)(adapters_of_tile(mt) * per_adapter);
+            st += skip;
+            if ((st / kStages) & 1u) ph ^= 1u;
+            st %= kStages;
+        }
+        // the completions of the last MMAs arrive here before the CTA may go away
+        for (int s = 0; s < kStages && ok; ++s) {
+            ok = tc::wait_bar_warp(bar_empty + 8 * st, ph ^ 1u, flags);
+            if (++st == kStages) { st = 0; ph ^= 1u; }
+        }
+        if (!ok) wide::outwait_copies();
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---- MMA issuer: the first CTA's, for both ----------------------------------------------------------
+        if (rank == 0) {
+            const bool leader = ptx::elect_one();
+            const uint64_t d_128 = tc::smem_desc(0u, 128u);
+            const uint32_t a_lo0 = base >> 4, step = kStage >> 4, half = kHalfStage >> 4;
+            constexpr uint32_t f16_types = std::is_same<H, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u;
+            uint32_t st = 0, ph = 0, done = 0;
+            bool ok = true, waited = !p.chained;
+            auto wait_full = [&] {
+                uint32_t i = 0;
+                unsigned long long t0 = 0;
+                bool there;
+                while (!(there = ptx::mbar_try_wait_cluster(bar_full + 8 * st, ph)))
+                    if ((++i & 1023u) == 0 && (t0 = tc::wait_check(t0, flags, tc::kWaitLimitNs)) == tc::kWaitGiveUp) break;
+                return (bool)__all_sync(0xFFFFFFFFu, there);
+            };
+            for (long long u = pair; u < units && ok; u += pairs, ++done) {
+                const int mt = (int)(u / q.n_ctiles), ct = (int)(u % q.n_ctiles);
+                const uint32_t shape = (((uint32_t)width(ct) >> 3) << 17) | ((256u >> 4) << 24);
+                const uint32_t id_i8 = (2u << 4) | (1u << 7) | (1u << 10) | shape, id_f16 = (1u << 4) | f16_types | shape;
+                if (!tc::wait_bar_warp(bar_tempty, (done & 1u) ^ 1u, flags)) { ok = false; break; }
+                ptx::tc_fence_after_sync();
+                for (int c = 0; c < q.kc; ++c) {
+                    if (!wait_full()) { ok = false; break; }
+                    ptx::tc_fence_after_sync();
+                    const uint32_t a_lo = a_lo0 + st * step, b_lo = a_lo + half;
+                    const int nks = c == q.kc - 1 ? q.ksteps_last : 4;
+                    if (leader) {
+                        if (c == 0) ptx::mma_i8_pair<false>(tmem, d_128 | (uint64_t)a_lo, d_128 | (uint64_t)b_lo, id_i8);
+                        else ptx::mma_i8_pair<true>(tmem, d_128 | (uint64_t)a_lo, d_128 | (uint64_t)b_lo, id_i8);
+#pragma unroll
+                        for (int ks = 1; ks < 4; ++ks)
+                            if (ks < nks)
+                                ptx::mma_i8_pair<true>(tmem, d_128 | (uint64_t)(a_lo + 2 * ks), d_128 | (uint64_t)(b_lo + 2 * ks), id_i8);
+                        ptx::mma_commit_pair(bar_empty + 8 * st);
+                    }
+                    if (++st == kStages) { st = 0; ph ^= 1u; }
+                }
+                if (ok && p.a) {
+                    if (!waited) { ptx::grid_dep_wait(); waited = true; }
+                    const int chunks = adapters_of_tile(mt) * per_adapter;
+                    for (int c = 0, part = 0; c < chunks; ++c) {
+                        if (!wait_full()) { ok = false; break; }
+                        ptx::tc_fence_after_sync();
+                        const uint32_t a_lo = a_lo0 + st * step, b_lo = a_lo + half;
+                        const int left = (k2 - 64 * part) >> 4, nks = left < 4 ? left : 4;
+                        if (leader) {
+                            for (int ks = 0; ks < nks; ++ks)
+                                ptx::mma_f16_pair(tmem + kD2, d_128 | (uint64_t)(a_lo + 2 * ks), d_128 | (uint64_t)(b_lo + 2 * ks), id_f16,
+                                                  c || ks ? 1u : 0u);
+                            ptx::mma_commit_pair(bar_empty + 8 * st);
+                        }
+                        if (++part == per_adapter) part = 0;
+                        if (++st == kStages) { st = 0; ph ^= 1u; }
+                    }
+                }
+                if (ok && leader) ptx::mma_commit_pair(bar_tfull);
+            }
+            // the second CTA's read-outs arrive here
+            if (ok && done) tc::wait_bar_warp(bar_tempty, (done & 1u) ^ 1u, flags);
+            if (leader) ptx::mma_commit_own(bar_drain);
+            const unsigned long long t0 = ptx::globaltimer();
+            while (!ptx::mbar_try_wait(bar_drain, 0) && ptx::globaltimer() - t0 < tc::kWaitLimitNs) {}
+        }
+        __syncwarp();
+    } else if (warp < kEpi0) {
+        // ---- fillers: weights, then the adapters' operands ----------------------------------------------------
+        const int f = threadIdx.x - 32 * kFill0, row = f >> 1, half = f & 1;        // half a row of 128 bytes
+        const uint32_t full = ptx::map_to_rank(bar_full, 0);
+        const int rowb = p.cin >> 2;
+        const bool wide_codes = (rowb & 15) == 0;
+        uint32_t st = 0, ph = 0, invalid = 0;
+        bool ok = true, waited = !p.chained, bad = false;
+        auto publish = [&](uint32_t arrivals) {
+            ptx::fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0)
+                for (uint32_t i = 0; i < arrivals; ++i) ptx::mbar_arrive_cluster_release(full + 8 * st);
+            if (++st == kStages) { st = 0; ph ^= 1u; }
+        };
+        for (long long u = pair; u < units && ok; u += pairs) {
+            const int mt = (int)(u / q.n_ctiles), ct = (int)(u % q.n_ctiles);
+            const int rows = width(ct) / 2, o = ct * q.nt + (int)rank * rows + row;
+            const bool mine = row < rows, there = mine && o < p.cout;
+            const uint8_t *src = p.w + (size_t)(there ? o : 0) * rowb + half * 16;
+            uint32_t code[kAhead][4];
+            auto fetch = [&](uint32_t (&v)[4], int c) {
+                const int k = c * 128 + half * 64;
+                if (wide_codes && there && k < p.cin) {
+                    const uint4 w = __ldg(reinterpret_cast<const uint4 *>(src + c * 32));
+                    v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = there && k + 16 * i < p.cin ? __ldg(reinterpret_cast<const uint32_t *>(src + c * 32) + i) : 0u;
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (i < q.kc) fetch(code[i], i);
+            for (int c0 = 0; c0 < q.kc && ok; c0 += kAhead) {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const int c = c0 + i;
+                    if (c >= q.kc) break;
+                    if (!tc::wait_bar_warp(bar_empty + 8 * st, ph ^ 1u, flags)) { ok = false; break; }
+                    uint8_t *dst = smem + st * kStage + kHalfStage;
+                    if (mine) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            invalid |= (code[i][j] >> 1) & ~code[i][j] & 0x55555555u;
+                            *reinterpret_cast<uint4 *>(dst + tc::swz_offset((uint32_t)row, (uint32_t)(half * 4 + j), 128u)) = expand_16(code[i][j]);
+                        }
+                    }
+                    if (c + kAhead < q.kc) fetch(code[i], c + kAhead);
+                    publish(1);
+                }
+            }
+            if (!ok || !p.a) continue;
+            if (!waited) { ptx::grid_dep_wait(); waited = true; }
+            const int adapters = adapters_of_tile(mt);
+            const long long r = (long long)mt * kTile + (int)rank * 128 + row;
+            int mine_a = -1;
+            const float *t = p.t;
+            float power = 1.0f;
+            if (adapters && r < p.m) {
+                mine_a = __ldg(p.which + r / p.rows_per_sample);
+                if (mine_a < 0 || mine_a >= p.n) mine_a = -1;
+                if (mine_a >= 0) { t = p.t + r * pitch; power = 1.0f / row_power(t, pitch); }
+            }
+            for (int i = 0; i < adapters && ok; ++i) {
+                const int a = __ldcg(p.list + (size_t)mt * kListInts + 1 + i);
+                const H *b = static_cast<const H *>(p.b) + ((size_t)a * p.cout + (there ? o : 0)) * p.rank;
+                for (int c = 0; c < per_adapter; ++c) {
+                    if (!tc::wait_bar_warp(bar_empty + 8 * st, ph ^ 1u, flags)) { ok = false; break; }
+                    uint8_t *dst = smem + st * kStage;
+#pragma unroll 1
+                    for (int k = 0; k < 4; ++k) {
+                        const int e = c * 64 + half * 32 + 8 * k, term = e / pitch, j = e - term * pitch;     // (pitch is a multiple of 16)
+                        const uint32_t off = tc::swz_offset((uint32_t)row, (uint32_t)(half * 4 + k), 128u);
+                        uint4 av = make_uint4(0u, 0u, 0u, 0u), bv = av;
+                        if (e < k2 && mine_a == a) {
+                            const float4 t0 = *reinterpret_cast<const float4 *>(t + j), t1 = *reinterpret_cast<const float4 *>(t + j + 4);
+                            float v[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
+#pragma unroll
+                            for (int s = 0; s < 8; ++s) {
+                                v[s] *= power;
+                                for (int m = 0; m < term; ++m) v[s] -= norm::to_float(norm::from_float<H>(v[s]));
+                            }
+                            av = make_uint4(pack_pair<H>(v[0], v[1]), pack_pair<H>(v[2], v[3]), pack_pair<H>(v[4], v[5]), pack_pair<H>(v[6], v[7]));
+                        }
+                        if (e < k2 && there && j < p.rank) {
+                            uint32_t w[4] = {0u, 0u, 0u, 0u};
+                            if ((p.rank & 7) == 0) {
+                                const uint4 v = __ldg(reinterpret_cast<const uint4 *>(b + j));
+                                w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+                            } else {
+                                for (int s = 0; s < 8; ++s)
+                                    if (j + s < p.rank) w[s >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short *>(b) + j + s) << (16 * (s & 1));
+                            }
+                            constexpr uint32_t top = std::is_same<H, __nv_bfloat16>::value ? 0x7F80u : 0x7C00u;    // the exponent of what is not finite
+#pragma unroll
+                            for (int s = 0; s < 4; ++s) {
+                                if ((w[s] & top) == top) { w[s] &= 0xFFFF0000u; bad = true; }
+                                if (((w[s] >> 16) & top) == top) { w[s] &= 0x0000FFFFu; bad = true; }
+                            }
+                            bv = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                        *reinterpret_cast<uint4 *>(dst + off) = av;
+                        if (mine) *reinterpret_cast<uint4 *>(dst + kHalfStage + off) = bv;
+                    }
+                    publish(warp == kFill0 && rank == 0 ? 2u : 1u);     // (the loader's arrival among them)
+                }
+            }
+        }
+        if (invalid || bad) raise_status(PROM_ERR_BAD_WEIGHT);
+        __syncwarp();
+    } else {
+        // ---- epilogue --------------------------------------------------------------------------------------------
+        // Two groups of four warps, a warp per quarter of the rows: pieces of 32 outputs, every second one a group's.
+        const int e = warp - kEpi0, quarter = warp & 3, grp = e >> 2;
+        uint8_t *slab = smem + kOffSlab + (size_t)e * kSlab;
+        const uint32_t slab_addr = ptx::smem_u32(slab);
+        const uint32_t t_lane = tmem + ((uint32_t)(quarter * 32) << 16);
+        const uint32_t tempty = ptx::map_to_rank(bar_tempty, 0);
+        constexpr uint32_t kRowBytes = 32u * (uint32_t)sizeof(Y);
+        if (p.chained) ptx::grid_dep_wait();
+        uint32_t done = 0;
+        for (long long u = pair; u < units; u += pairs, ++done) {
+            const int mt = (int)(u / q.n_ctiles), ct = (int)(u % q.n_ctiles), pieces = width(ct) / 32;
+            const long long row0 = (long long)mt * kTile + (int)rank * 128 + quarter * 32, r = row0 + lane;
+            const int adapters = adapters_of_tile(mt);
+            float fac = 0.0f, ad = 0.0f;
+            bool with = false;
+            if (r < p.m) {
+                const long long s = r / p.rows_per_sample;
+                fac = row_factor(p, s);
+                if (adapters) {
+                    const int a = __ldg(p.which + s);
+                    with = a >= 0 && a < p.n;
+                    if (with) ad = (p.scale ? __ldg(p.scale + a) : 1.0f) * fac * row_power(p.t + r * pitch, pitch);
+                }
+            }
+            if (!tc::wait_bar<true>(bar_tfull, done & 1u, flags)) break;
+            ptx::tc_fence_after_sync();
+            auto release = [&] {
+                ptx::tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive_cluster(tempty);
+            };
+            if (grp >= pieces) release();
+#pragma unroll 1
+            for (int pc = grp; pc < pieces; pc += 2) {
+                const int at = ct * q.nt + pc * 32;
+                uint32_t v[32], w[32];
+                ptx::tmem_ld_x32(t_lane + (uint32_t)pc * 32u, v);
+                if (adapters) ptx::tmem_ld_x32(t_lane + kD2 + (uint32_t)pc * 32u, w);
+                ptx::tmem_wait_ld();
+                if (pc + 2 >= pieces) release();
+                float y[32];
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    float4 al = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if (at + i < p.cout) {          // (whole groups of eight outputs)
+                        al.x = __ldg(p.alpha + at + i); al.y = __ldg(p.alpha + at + i + 1);
+                        al.z = __ldg(p.alpha + at + i + 2); al.w = __ldg(p.alpha + at + i + 3);
+                    }
+                    y[i] = (float)(int)v[i] * al.x * fac;
+                    y[i + 1] = (float)(int)v[i + 1] * al.y * fac;
+                    y[i + 2] = (float)(int)v[i + 2] * al.z * fac;
+                    y[i + 3] = (float)(int)v[i + 3] * al.w * fac;
+                }
+                if (with) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) y[i] += ad * __uint_as_float(w[i]);
+                }
+                ptx::bulk_wait_read0();             // the previous store has read the slab
+                __syncwarp();
+                if constexpr (sizeof(Y) == 4) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        *reinterpret_cast<float4 *>(slab + tc::swz_offset((uint32_t)lane, (uint32_t)j, 128u)) =
+                            make_float4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<uint4 *>(slab + tc::swz_offset((uint32_t)lane, (uint32_t)j, 64u)) =
+                            make_uint4(pack_pair<Y>(y[8 * j], y[8 * j + 1]), pack_pair<Y>(y[8 * j + 2], y[8 * j + 3]),
+                                       pack_pair<Y>(y[8 * j + 4], y[8 * j + 5]), pack_pair<Y>(y[8 * j + 6], y[8 * j + 7]));
+                }
+                if (q.store) {
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0 && row0 < p.m) {
+                        ptx::tma_store_2d(&ymap, at, (int)row0, slab_addr);
+                        ptx::bulk_commit();
+                    }
+                } else {
+                    __syncwarp();
+                    constexpr uint32_t per = 16u / (uint32_t)sizeof(Y);
+                    if (at + lane < p.cout)
+                        for (int i = 0; i < 32 && row0 + i < p.m; ++i)
+                            static_cast<Y *>(p.y)[(row0 + i) * p.y_pitch + at + lane] =
+                                *reinterpret_cast<const Y *>(slab + tc::swz_offset((uint32_t)i, (uint32_t)lane / per, kRowBytes) + (lane % per) * sizeof(Y));
+                    __syncwarp();
+                }
+            }
+        }
+        ptx::bulk_wait_all();
+    }
+
+    // neither CTA may go while the other can still reach its shared memory
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::cluster_sync();
+    if (warp == 1) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc_pair(tmem, 512u);
+    }
 }
 
 }}  // namespace prom::lora

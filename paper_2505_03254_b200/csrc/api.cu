@@ -2360,6 +2360,9 @@ namespace prom { namespace lora {
 
 constexpr int kMaxRank = 256;
 
+// 0: the library's choice, 1: the kernels for few rows, 2: the tiled ones (tests and timing).
+static std::atomic<int> g_adapters_mode{0};
+
 template <class H, class Y, int MO, int MT>
 static prom_status launch_rows(const Params &p, cudaStream_t st)
 {
@@ -2389,15 +2392,121 @@ static prom_status run_rows(Params &p, cudaStream_t st)
     return launch_rows<H, Y, 2, 4>(p, st);
 }
 
+// Pairs of CTAs of the tiled kernel that the device holds at once.
+template <class H, class Y>
+static int tile_pairs(const DeviceInfo &d)
+{
+    static std::atomic<int> known[64];
+    const bool keep = d.dev >= 0 && d.dev < 64;
+    int n = keep ? known[d.dev].load() : 0;
+    if (n == 0) {
+        if (raise_smem_limit(proj_tiles_kernel<H, Y>, (int)kTileSmem) != cudaSuccess) return 0;
+        cudaLaunchConfig_t cfg;
+        fill_launch_cfg(cfg, nullptr, 2 * (d.sms / 2), kTileThreads, kTileSmem, nullptr, false);
+        if (cudaOccupancyMaxActiveClusters(&n, proj_tiles_kernel<H, Y>, &cfg) != cudaSuccess) {
+            cudaGetLastError();
+            n = 0;
+        }
+        if (n > d.sms / 2) n = d.sms / 2;
+        if (keep) known[d.dev].store(n);
+    }
+    return n;
+}
+
+static long long row_tiles(long long m) { return (m + kTile - 1) / kTile; }
+static int pitch_of(int rank) { return (rank + 15) & ~15; }
+static size_t t_bytes(long long m, int rank) { return round256((size_t)m * pitch_of(rank) * sizeof(float)); }
+static size_t workspace_bytes(long long m, int rank)
+{
+    return t_bytes(m, rank) + round256((size_t)row_tiles(m) * kListInts * sizeof(int));
+}
+
+template <class H, class Y>
+static prom_status run_tiles(Params &p, int y_type, const DeviceInfo &d, cudaStream_t st)
+{
+    EncodeTiledFn enc = encode_tiled_fn();
+    const int pairs = tile_pairs<H, Y>(d);
+    if (!enc || pairs < 1) return PROM_ERR_CUDA;
+    Tiles q;
+    memset(&q, 0, sizeof(q));
+    q.kc = (p.cin + 127) / 128;
+    q.ksteps_last = (p.cin - 128 * (q.kc - 1) + 31) / 32;
+    q.n_mtiles = (int)row_tiles(p.m);
+    q.nt = 256;
+    while (q.nt > 64 && (long long)q.n_mtiles * ((p.cout + q.nt - 1) / q.nt) < pairs) q.nt /= 2;
+    q.n_ctiles = (p.cout + q.nt - 1) / q.nt;
+    q.terms = y_type == PROM_TYPE_F32 ? 3 : 2;
+    const size_t bytes = norm::type_bytes(y_type);
+    q.store = norm::whole_pieces(p.y, p.y_pitch, bytes);
+    CUtensorMap xmap, ymap;
+    cuuint32_t es[2] = {1, 1};
+    {
+        cuuint64_t dims[2] = {(cuuint64_t)p.cin, (cuuint64_t)p.m};
+        cuuint64_t strides[1] = {(cuuint64_t)p.cin};
+        cuuint32_t box[2] = {128, 128};
+        if (enc(&xmap, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t *>(p.x), dims, strides, box, es,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return PROM_ERR_CUDA;
+    }
+    ymap = xmap;
+    if (q.store) {
+        cuuint64_t dims[2] = {(cuuint64_t)p.cout, (cuuint64_t)p.m};
+        cuuint64_t strides[1] = {(cuuint64_t)p.y_pitch * bytes};
+        cuuint32_t box[2] = {32, 32};
+        const CUtensorMapDataType type = y_type == PROM_TYPE_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                         : y_type == PROM_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                                    : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+        if (enc(&ymap, type, 2, p.y, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                bytes == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
+            ymap = xmap;
+            q.store = 0;            // (a pitch that the map does not hold: plain stores)
+        }
+    }
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[1];
+    if (p.a) {
+        p.t_pitch = pitch_of(p.rank);
+        p.list = reinterpret_cast<int *>(reinterpret_cast<uint8_t *>(p.t) + t_bytes(p.m, p.rank));
+        if (raise_smem_limit(inner_tiles_kernel<H>, kInnerSmem) != cudaSuccess) return PROM_ERR_CUDA;
+        fill_launch_cfg(cfg, attr, 1, 32 * kInnerWarps, kInnerSmem, st, true);
+        // a tile's items over several blocks: four of a run of 256 rows, more where there are few tiles
+        const int zs = (p.t_pitch + 31) / 32;
+        long long share = (2ll * d.sms + (long long)q.n_mtiles * zs - 1) / ((long long)q.n_mtiles * zs);
+        share = share < 4 ? 4 : (share > 32 ? 32 : share);
+        cfg.gridDim = dim3((unsigned)q.n_mtiles, (unsigned)share, (unsigned)zs);
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, inner_tiles_kernel<H>, p);
+        ++g_launches;
+        if (e != cudaSuccess) return cuda_status(e);
+        p.chained = 1;
+    }
+    q.p = p;
+    const long long units = (long long)q.n_mtiles * q.n_ctiles;
+    fill_launch_cfg(cfg, attr, 2 * (int)(units < pairs ? units : pairs), kTileThreads, kTileSmem, st, true);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, proj_tiles_kernel<H, Y>, xmap, ymap, q);
+    ++g_launches;
+    return cuda_status(e);
+}
+
+template <class H, class Y>
+static prom_status run_as(Params &p, int y_type, const DeviceInfo &d, cudaStream_t st)
+{
+    const int mode = g_adapters_mode.load();
+    if (mode == 2 || (mode == 0 && p.m > 128)) return run_tiles<H, Y>(p, y_type, d, st);
+    p.t_pitch = p.rank;
+    return run_rows<H, Y>(p, st);
+}
+
 template <class H>
 static prom_status run(Params &p, int y_type, cudaStream_t st)
 {
-    if (y_type == PROM_TYPE_F32) return run_rows<H, float>(p, st);
-    if (y_type == PROM_TYPE_BF16) return run_rows<H, __nv_bfloat16>(p, st);
-    return run_rows<H, __half>(p, st);
+    DeviceInfo d = device_info();
+    if (!d.ok) return PROM_ERR_CUDA;
+    if (y_type == PROM_TYPE_F32) return run_as<H, float>(p, y_type, d, st);
+    if (y_type == PROM_TYPE_BF16) return run_as<H, __nv_bfloat16>(p, y_type, d, st);
+    return run_as<H, __half>(p, y_type, d, st);
 }
-
-static size_t workspace_bytes(long long m, int rank) { return round256((size_t)m * rank * sizeof(float)); }
 
 }}  // namespace prom::lora
 
@@ -3249,6 +3358,8 @@ void prom_debug_seq_block(int mode, int rows, int split)
     g_block_split.store(split);
 }
 void prom_debug_dw_variant(int variant) { g_dw_variant.store(variant < 0 || variant > 2 ? 0 : variant); }
+
+void prom_debug_adapters(int mode) { lora::g_adapters_mode.store(mode < 0 || mode > 2 ? 0 : mode); }
 
 void prom_debug_tc_wide(int mode, int blocks)
 {

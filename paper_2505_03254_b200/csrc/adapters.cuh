@@ -25,9 +25,13 @@ struct Params {
     int n, rank;
     void *y;
     long long y_pitch;
-    float *t;                       // [m][t_pitch] inner products
-    int t_pitch;                    // rank, or rounded up to 16 with zeros behind it (many rows)
-    int *list;                      // many rows: per tile of 256 rows the number of its adapters and these
+    float *t;                       // [m][rank] inner products (few rows)
+    // Many rows: the inner products as sums of `terms` 16-bit values, [m][terms][pitch] (pitch: rank rounded up to 16, zeros
+    // behind it), divided by a power of two per row; and per tile of 256 rows the number of its adapters and these.
+    void *t16;
+    float *power;
+    int *list;
+    int pitch, terms;
     int chained;                    // a kernel of the same call is in front: only what that one writes is waited for
 };
 
@@ -85,7 +89,7 @@ inner_rows_kernel(const Params p)
         }
     }
     sum = norm::warp_sum(sum);
-    if (lane == 0) p.t[r * p.t_pitch + j] = sum;
+    if (lane == 0) p.t[r * p.rank + j] = sum;
 }
 
 // sum_j B[a][o][j] t[j].  A value of B that is not finite counts as zero and is reported (many rows share a tile of B,
@@ -240,7 +244,7 @@ proj_rows_kernel(const Params p)
         const float f = row_factor(p, s);
         float y = (float)acc * __ldg(p.alpha + o0 + o) * f;
         const int a = adapter_of(p, s);
-        if (a >= 0) y += (p.scale ? __ldg(p.scale + a) : 1.0f) * f * outer<H>(p, a, o0 + o, p.t + r * p.t_pitch, bad);
+        if (a >= 0) y += (p.scale ? __ldg(p.scale + a) : 1.0f) * f * outer<H>(p, a, o0 + o, p.t + r * p.rank, bad);
         static_cast<Y *>(p.y)[r * p.y_pitch + o0 + o] = norm::from_float<Y>(y);
     }
     if (bad) raise_status(PROM_ERR_BAD_WEIGHT);
@@ -248,14 +252,16 @@ proj_rows_kernel(const Params p)
 
 // ---- many rows: inner products ----------------------------------------------------------------------------------
 // Rows in tiles of 256.  A block sorts the tile's rows by their adapter (each thread counts the rows that come before its
-// own), so that any order of requests costs what runs of requests cost: an item is up to 64 rows of one adapter, found
-// by index.  Items go round the blocks of a tile, ranks in parts of 32 over blockIdx.z.  The eight warps share K and
-// multiply with the warp-level 16-bit MMA, rows as A (int8 values are exact in both 16-bit types) and the adapter as B; a
-// thread's 16 bytes of a row and 32 of the adapter are 16 neighbouring values of k, whose order inside the MMAs is free.
+// own), so that any order of requests costs what runs of requests cost: an item is up to 32 rows of one adapter, found
+// by index, and the items go round the blocks of a tile.  The eight warps share K and multiply with the warp-level
+// 16-bit MMA, rows as A (int8 values are exact in both 16-bit types) and the adapter as B; a thread's 16 bytes of a row and
+// 32 of the adapter are 16 neighbouring values of k, whose order inside the MMAs is free.  The sums are then split into
+// 16-bit values once, for all the projection's tiles of outputs.
 constexpr int kTile = 256;
-constexpr int kItemRows = 64;
+constexpr int kItemRows = 32;
 constexpr int kListInts = kTile + 1;
 constexpr int kInnerWarps = 8;
+constexpr int kRankPart = 64;               // ranks of one pass over K
 
 // Four int8 values (one word) to two words of 16-bit values: 0, 1 and 2, 3.
 template <class H> __device__ __forceinline__ void widen_4(uint32_t w, uint32_t &lo, uint32_t &hi);
@@ -292,15 +298,39 @@ template <> __device__ __forceinline__ void mma_16<__half>(float (&d)[4], const 
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Partial sums of an item: [rows][32 ranks] per warp.
-constexpr int kInnerSmem = kInnerWarps * kItemRows * 33 * (int)sizeof(float);
+template <class H> __device__ __forceinline__ uint32_t pack_pair(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack_pair<__nv_bfloat16>(float lo, float hi)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+template <> __device__ __forceinline__ uint32_t pack_pair<__half>(float lo, float hi)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// The power of two by which a row's inner products are divided, so that the largest lies in [2^13, 2^14): far from both ends
+// of the 16-bit types.  1 for a row of (nearly) zeros or one that has a value which is not finite.
+__device__ __forceinline__ float row_power(float top)
+{
+    const uint32_t e = (__float_as_uint(top) >> 23) & 0xFFu;
+    return e <= 14u || e == 255u ? 1.0f : __uint_as_float((e - 13u) << 23);
+}
+
+// Shared memory: partial sums [warp][row][kRankPart + 1], then the item's sums [row][pitch].
+constexpr int kPartPitch = kRankPart + 1;
+constexpr int kPartFloats = kInnerWarps * kItemRows * kPartPitch;
+static inline size_t inner_smem(int pitch) { return (size_t)(kPartFloats + kItemRows * pitch) * sizeof(float); }
 
 template <class H>
 __global__ void __launch_bounds__(32 * kInnerWarps)
 inner_tiles_kernel(const Params p)
 {
-    extern __shared__ float part[];             // [warp][row][33]
-    __shared__ int key_s[kTile], row_s[kTile];  // adapters by row; rows in the order of their adapters
+    extern __shared__ float part[];
+    float *sums = part + kPartFloats;
+    __shared__ __align__(16) int key_s[kTile];
+    __shared__ int row_s[kTile];                // rows in the order of their adapters
     __shared__ int item_s[kTile];               // first place | rows << 16
     __shared__ int warp_items[kTile / 32], warp_lists[kTile / 32];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -313,15 +343,20 @@ inner_tiles_kernel(const Params p)
     key_s[tid] = key;
     __syncthreads();
     int less = 0, same_before = 0, same = 0;
-    for (int i = 0; i < kTile; ++i) {
-        const int k = key_s[i];
-        less += k >= 0 && k < key;
-        same += k == key;
-        same_before += k == key && i < tid;
+#pragma unroll 4
+    for (int i = 0; i < kTile; i += 4) {
+        const int4 k4 = *reinterpret_cast<const int4 *>(key_s + i);
+        const int k[4] = {k4.x, k4.y, k4.z, k4.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            less += k[e] >= 0 && k[e] < key;
+            same += k[e] == key;
+            same_before += k[e] == key && i + e < tid;
+        }
     }
     const int place = less + same_before;
     if (key >= 0) row_s[place] = tid;
-    // an item starts at every 64th row of an adapter; the list of adapters has their first rows
+    // an item starts at every 32nd row of an adapter; the list of adapters has their first rows
     const bool head = key >= 0 && same_before % kItemRows == 0, newcomer = key >= 0 && same_before == 0;
     const unsigned heads = __ballot_sync(0xFFFFFFFFu, head), news = __ballot_sync(0xFFFFFFFFu, newcomer);
     if (lane == 0) { warp_items[warp] = __popc(heads); warp_lists[warp] = __popc(news); }
@@ -337,83 +372,113 @@ inner_tiles_kernel(const Params p)
         const int left = same - same_before;
         item_s[before + __popc(heads & below)] = place | ((left < kItemRows ? left : kItemRows) << 16);
     }
-    if (blockIdx.y == 0 && blockIdx.z == 0) {
+    if (blockIdx.y == 0) {
         int *list = p.list + tile * kListInts;
         if (newcomer) list[1 + list_before + __popc(news & below)] = key;
         if (tid == 0) list[0] = adapters;
     }
     __syncthreads();
 
-    const int j0 = blockIdx.z * 32, ranks = p.t_pitch - j0 < 32 ? p.t_pitch - j0 : 32;      // a multiple of 16
     for (int it = blockIdx.y; it < items; it += gridDim.y) {
         const int at = item_s[it] & 0xFFFF, count = item_s[it] >> 16;
         const int a = key_s[row_s[at]];
         const H *am = static_cast<const H *>(p.a) + (size_t)a * p.rank * p.cin;
-        float acc[4][4][4];                     // [16 rows][8 ranks][...]
+        const int8_t *xr[2][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
-        const int8_t *xr[4][2];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int k = 16 * i + 8 * h + g;
                 xr[i][h] = p.x + (first + row_s[at + (k < count ? k : 0)]) * p.cin;
             }
-        for (int k = warp * 64 + 16 * t; k < ((p.cin + 63) & ~63); k += 64 * kInnerWarps) {
-            const bool in = k < p.cin;
-            uint32_t b[4][8];
+        for (int j0 = 0; j0 < p.pitch; j0 += kRankPart) {
+            const int ranks = p.pitch - j0 < kRankPart ? p.pitch - j0 : kRankPart;      // a multiple of 16
+            float acc[2][8][4];                 // [16 rows][8 ranks][...]
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int rk = j0 + 8 * j + g;
-                uint4 v0 = make_uint4(0u, 0u, 0u, 0u), v1 = v0;
-                if (8 * j < ranks && in && rk < p.rank) {
-                    const uint4 *src = reinterpret_cast<const uint4 *>(am + (size_t)rk * p.cin + k);
-                    v0 = __ldg(src); v1 = __ldg(src + 1);
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
+            for (int k = warp * 64 + 16 * t; k < ((p.cin + 63) & ~63); k += 64 * kInnerWarps) {
+                const bool in = k < p.cin;
+                uint32_t xw[2][2][4];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                        if (in && 16 * i < count) v = __ldg(reinterpret_cast<const uint4 *>(xr[i][h] + k));
+                        xw[i][h][0] = v.x; xw[i][h][1] = v.y; xw[i][h][2] = v.z; xw[i][h][3] = v.w;
+                    }
+#pragma unroll
+                for (int jj = 0; jj < 8; jj += 4) {
+                    if (8 * jj >= ranks) break;
+                    uint32_t b[4][8];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int rk = j0 + 8 * (jj + j) + g;
+                        uint4 v0 = make_uint4(0u, 0u, 0u, 0u), v1 = v0;
+                        if (in && rk < p.rank) {
+                            const uint4 *src = reinterpret_cast<const uint4 *>(am + (size_t)rk * p.cin + k);
+                            v0 = __ldg(src); v1 = __ldg(src + 1);
+                        }
+                        b[j][0] = v0.x; b[j][1] = v0.y; b[j][2] = v0.z; b[j][3] = v0.w;
+                        b[j][4] = v1.x; b[j][5] = v1.y; b[j][6] = v1.z; b[j][7] = v1.w;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if (16 * i >= count) break;
+#pragma unroll
+                        for (int s = 0; s < 4; ++s) {
+                            uint32_t f[4];
+                            widen_4<H>(xw[i][0][s], f[0], f[2]);
+                            widen_4<H>(xw[i][1][s], f[1], f[3]);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                if (8 * (jj + j) < ranks) mma_16<H>(acc[i][jj + j], f, b[j][2 * s], b[j][2 * s + 1]);
+                        }
+                    }
                 }
-                b[j][0] = v0.x; b[j][1] = v0.y; b[j][2] = v0.z; b[j][3] = v0.w;
-                b[j][4] = v1.x; b[j][5] = v1.y; b[j][6] = v1.z; b[j][7] = v1.w;
             }
+            float *mine = part + (size_t)warp * kItemRows * kPartPitch;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 2; ++i) {
                 if (16 * i >= count) break;
-                uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
-                if (in) {
-                    lo = __ldg(reinterpret_cast<const uint4 *>(xr[i][0] + k));
-                    hi = __ldg(reinterpret_cast<const uint4 *>(xr[i][1] + k));
-                }
-                const uint32_t lw[4] = {lo.x, lo.y, lo.z, lo.w}, hw[4] = {hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    uint32_t f[4];
-                    widen_4<H>(lw[s], f[0], f[2]);
-                    widen_4<H>(hw[s], f[1], f[3]);
+                for (int j = 0; j < 8; ++j)
+                    if (8 * j < ranks) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (8 * j < ranks) mma_16<H>(acc[i][j], f, b[j][2 * s], b[j][2 * s + 1]);
+                        for (int e = 0; e < 4; ++e) mine[(16 * i + g + 8 * (e >> 1)) * kPartPitch + 8 * j + 2 * t + (e & 1)] = acc[i][j][e];
+                    }
+            }
+            __syncthreads();
+            for (int i = tid; i < count * ranks; i += 32 * kInnerWarps) {
+                const int k = i / ranks, j = i - k * ranks;
+                float s = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kInnerWarps; ++w) s += part[(w * kItemRows + k) * kPartPitch + j];
+                sums[k * p.pitch + j0 + j] = s;
+            }
+            __syncthreads();
+        }
+        // a warp per row: the power, and the 16-bit values
+        for (int k = warp; k < count; k += kInnerWarps) {
+            const float *v = sums + k * p.pitch;
+            float top = 0.0f;
+            for (int j = lane; j < p.pitch; j += 32) top = norm::max_nan(top, fabsf(v[j]));
+            const float power = row_power(norm::warp_max(top)), by = 1.0f / power;
+            const long long r = first + row_s[at + k];
+            if (lane == 0) p.power[r] = power;
+            uint32_t *out = static_cast<uint32_t *>(p.t16) + (size_t)r * p.terms * (p.pitch / 2);
+            for (int j = lane; j < p.pitch / 2; j += 32) {
+                float lo = v[2 * j] * by, hi = v[2 * j + 1] * by;
+                for (int m = 0; m < p.terms; ++m) {
+                    out[m * (p.pitch / 2) + j] = pack_pair<H>(lo, hi);
+                    lo -= norm::to_float(norm::from_float<H>(lo));
+                    hi -= norm::to_float(norm::from_float<H>(hi));
                 }
             }
-        }
-        float *mine = part + (size_t)warp * kItemRows * 33;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (16 * i >= count) break;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) mine[(16 * i + g + 8 * (e >> 1)) * 33 + 8 * j + 2 * t + (e & 1)] = acc[i][j][e];
-        }
-        __syncthreads();
-        for (int i = tid; i < count * ranks; i += 32 * kInnerWarps) {
-            const int k = i / ranks, j = i - k * ranks;
-            float s = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kInnerWarps; ++w) s += part[((size_t)w * kItemRows + k) * 33 + j];
-            p.t[(first + row_s[at + k]) * p.t_pitch + j0 + j] = s;
         }
         __syncthreads();
     }
@@ -423,12 +488,12 @@ inner_tiles_kernel(const Params p)
 // Tiles of 256 rows x nt outputs by pairs of CTAs (cta_group::2, 128 rows of x and half of the tile's weights in each),
 // two accumulators in tensor memory: int32 for the projection, binary32 for the adapters, which the epilogue joins.
 // x comes by TMA.  The weights never exist as bytes in memory: eight warps expand the 2-bit codes into the swizzled
-// operand layout on their way into shared memory, so a stage takes 4 KB of weights from L2 instead of 16 (a pair's SM would
+// operand layout on their way into shared memory (four pairs of warps take the stages in turn), so a stage takes 4 KB of weights from L2 instead of 16 (a pair's SM would
 // need 64 bytes a clock of both operands at the MMAs' rate, of the 58 that L2 gives it; this way it is 40).
 // Behind the chunks of K come those of the adapters: for each adapter of the tile the rows' inner products (zero for rows of
 // other adapters), as sums of 16-bit values (two, or three for binary32 outputs) side by side along K, against B
-// repeated as often.  A row's products are first scaled by a power of two so that they fit the 16-bit type.
-constexpr int kFillWarps = 8, kEpiWarps = 8;
+// repeated as often.
+constexpr int kFillGroups = 4, kGroupWarps = 2, kFillWarps = kFillGroups * kGroupWarps, kEpiWarps = 8;
 constexpr int kFill0 = 2, kEpi0 = kFill0 + kFillWarps;
 constexpr int kTileThreads = 32 * (kEpi0 + kEpiWarps);
 constexpr int kStages = 6;
@@ -438,13 +503,11 @@ constexpr uint32_t kOffSlab = kStages * kStage;
 constexpr uint32_t kOffBars = kOffSlab + kEpiWarps * kSlab;
 constexpr size_t kTileSmem = 1024 + kOffBars + 256;
 constexpr uint32_t kD2 = 256;               // column of the adapters' accumulator
-constexpr int kAhead = 4;                   // chunks of codes in registers
 
 struct Tiles {
     Params p;
     int kc, ksteps_last;        // chunks of 128 bytes of K; MMA steps in the last one
     int n_mtiles, n_ctiles, nt;
-    int terms;                  // 16-bit values per inner product
     int store;                  // y has a tensor map
 };
 
@@ -455,31 +518,6 @@ __device__ __forceinline__ uint4 expand_16(uint32_t w)
     const uint32_t e0 = __byte_perm(lut, 0u, even), e1 = __byte_perm(lut, 0u, even >> 16);
     const uint32_t o0 = __byte_perm(lut, 0u, odd), o1 = __byte_perm(lut, 0u, odd >> 16);
     return make_uint4(__byte_perm(e0, o0, 0x5140), __byte_perm(e0, o0, 0x7362), __byte_perm(e1, o1, 0x5140), __byte_perm(e1, o1, 0x7362));
-}
-
-template <class H> __device__ __forceinline__ uint32_t pack_pair(float lo, float hi);
-template <> __device__ __forceinline__ uint32_t pack_pair<__nv_bfloat16>(float lo, float hi)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-template <> __device__ __forceinline__ uint32_t pack_pair<__half>(float lo, float hi)
-{
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-
-// The power of two by which a row's inner products are divided, so that the largest lies in [2^13, 2^14): far from both ends
-// of the 16-bit types.  1 for a row of (nearly) zeros or one that has a value which is not finite.
-__device__ __forceinline__ float row_power(const float *t, int n)
-{
-    float top = 0.0f;
-    for (int j = 0; j < n; j += 4) {
-        const float4 v = *reinterpret_cast<const float4 *>(t + j);
-        top = norm::max_nan(norm::max_nan(top, fabsf(v.x)), norm::max_nan(fabsf(v.y), norm::max_nan(fabsf(v.z), fabsf(v.w))));
-    }
-    const uint32_t e = (__float_as_uint(top) >> 23) & 0xFFu;
-    return e <= 14u || e == 255u ? 1.0f : __uint_as_float((e - 13u) << 23);
 }
 
 template <class H, class Y>
@@ -504,11 +542,11 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
     const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
     const long long units = (long long)q.n_mtiles * q.n_ctiles;
     auto width = [&](int ct) { const int left = p.cout - ct * q.nt; return left >= q.nt ? q.nt : (left + 31) & ~31; };
-    const int pitch = p.t_pitch, k2 = q.terms * pitch, per_adapter = (k2 + 63) >> 6;    // chunks of 64 values
+    const int k2 = p.terms * p.pitch, per_adapter = (k2 + 63) >> 6;    // chunks of 64 values
 
     if (warp == 0) {
         if (lane < kStages) {
-            ptx::mbar_init(bar_full + 8 * lane, 1 + 2 * kFillWarps);
+            ptx::mbar_init(bar_full + 8 * lane, 1 + 2 * kGroupWarps);
             ptx::mbar_init(bar_empty + 8 * lane, 1);
         } else if (lane == 31) {
             ptx::mbar_init(bar_tfull, 1);
@@ -548,12 +586,13 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                 if (++st == kStages) { st = 0; ph ^= 1u; }
             }
             if (!ok || !p.a) continue;
-            // the adapters' stages are the fillers' alone
+            // The adapters' stages are the fillers' alone, but each is waited for: a wait for a phase can not be told
+            // from one for the phase two before it.
             if (!waited) { ptx::grid_dep_wait(); waited = true; }
-            const uint32_t skip = (uint32_t)(adapters_of_tile(mt) * per_adapter);
-            st += skip;
-            if ((st / kStages) & 1u) ph ^= 1u;
-            st %= kStages;
+            for (int c = adapters_of_tile(mt) * per_adapter; c > 0 && ok; --c) {
+                ok = tc::wait_bar_warp(bar_empty + 8 * st, ph ^ 1u, flags);
+                if (++st == kStages) { st = 0; ph ^= 1u; }
+            }
         }
         // the completions of the last MMAs arrive here before the CTA may go away
         for (int s = 0; s < kStages && ok; ++s) {
@@ -571,14 +610,7 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
             constexpr uint32_t f16_types = std::is_same<H, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u;
             uint32_t st = 0, ph = 0, done = 0;
             bool ok = true, waited = !p.chained;
-            auto wait_full = [&] {
-                uint32_t i = 0;
-                unsigned long long t0 = 0;
-                bool there;
-                while (!(there = ptx::mbar_try_wait_cluster(bar_full + 8 * st, ph)))
-                    if ((++i & 1023u) == 0 && (t0 = tc::wait_check(t0, flags, tc::kWaitLimitNs)) == tc::kWaitGiveUp) break;
-                return (bool)__all_sync(0xFFFFFFFFu, there);
-            };
+            auto wait_full = [&] { return tc::wait_bar_warp(bar_full + 8 * st, ph, flags); };
             for (long long u = pair; u < units && ok; u += pairs, ++done) {
                 const int mt = (int)(u / q.n_ctiles), ct = (int)(u % q.n_ctiles);
                 const uint32_t shape = (((uint32_t)width(ct) >> 3) << 17) | ((256u >> 4) << 24);
@@ -630,112 +662,134 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
         __syncwarp();
     } else if (warp < kEpi0) {
         // ---- fillers: weights, then the adapters' operands ----------------------------------------------------
-        const int f = threadIdx.x - 32 * kFill0, row = f >> 1, half = f & 1;        // half a row of 128 bytes
+        // The stages of all units are numbered through, a group takes every fourth.  A thread has four half rows of
+        // 64 bytes: rows row0, row0 + 32, ...
+        const int f = threadIdx.x - 32 * kFill0, grp = f / (32 * kGroupWarps), ft = f % (32 * kGroupWarps);
+        const int row0 = ft >> 1, half = ft & 1;
         const uint32_t full = ptx::map_to_rank(bar_full, 0);
         const int rowb = p.cin >> 2;
         const bool wide_codes = (rowb & 15) == 0;
-        uint32_t st = 0, ph = 0, invalid = 0;
+        uint32_t seq = 0, invalid = 0;          // number of the unit's first stage
         bool ok = true, waited = !p.chained, bad = false;
-        auto publish = [&](uint32_t arrivals) {
+        auto enter = [&](uint32_t n) {
+            return tc::wait_bar_warp(bar_empty + 8 * (n % kStages), ((n / kStages) & 1u) ^ 1u, flags);
+        };
+        // The operands that the arrival announces are read by the tensor cores of the SM that wrote them, and this SM's fence
+        // stands before it: what crosses to the first CTA is the signal alone.  (With release.cluster the arrival waits
+        // some hundred clocks for stores that nobody there reads: 148 us instead of 115 at 8192 rows 4096 -> 4096.)
+        auto publish = [&](uint32_t n, uint32_t arrivals) {
             ptx::fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0)
-                for (uint32_t i = 0; i < arrivals; ++i) ptx::mbar_arrive_cluster_release(full + 8 * st);
-            if (++st == kStages) { st = 0; ph ^= 1u; }
+                for (uint32_t i = 0; i < arrivals; ++i) ptx::mbar_arrive_cluster(full + 8 * (n % kStages));
         };
         for (long long u = pair; u < units && ok; u += pairs) {
             const int mt = (int)(u / q.n_ctiles), ct = (int)(u % q.n_ctiles);
-            const int rows = width(ct) / 2, o = ct * q.nt + (int)rank * rows + row;
-            const bool mine = row < rows, there = mine && o < p.cout;
-            const uint8_t *src = p.w + (size_t)(there ? o : 0) * rowb + half * 16;
-            uint32_t code[kAhead][4];
-            auto fetch = [&](uint32_t (&v)[4], int c) {
+            const int rows = width(ct) / 2, o0 = ct * q.nt + (int)rank * rows;
+            uint32_t code[4][4];
+            auto fetch = [&](int c) {
                 const int k = c * 128 + half * 64;
-                if (wide_codes && there && k < p.cin) {
-                    const uint4 w = __ldg(reinterpret_cast<const uint4 *>(src + c * 32));
-                    v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
-                } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = there && k + 16 * i < p.cin ? __ldg(reinterpret_cast<const uint32_t *>(src + c * 32) + i) : 0u;
+                for (int i = 0; i < 4; ++i) {
+                    const int row = row0 + 32 * i;
+                    const bool there = row < rows && o0 + row < p.cout;
+                    const uint8_t *src = p.w + (size_t)(there ? o0 + row : 0) * rowb + c * 32 + half * 16;
+                    if (wide_codes) {
+                        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                        if (there && k < p.cin) w = __ldg(reinterpret_cast<const uint4 *>(src));
+                        code[i][0] = w.x; code[i][1] = w.y; code[i][2] = w.z; code[i][3] = w.w;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            code[i][j] = there && k + 16 * j < p.cin ? __ldg(reinterpret_cast<const uint32_t *>(src) + j) : 0u;
+                    }
                 }
             };
+            int c = (int)(((uint32_t)grp - seq) % kFillGroups);
+            if (c < q.kc) fetch(c);
+            for (; c < q.kc; c += kFillGroups) {
+                const uint32_t n = seq + (uint32_t)c;
+                // expanded while the stage is still in use: only the stores are behind the wait
+                uint4 wide[4][4];
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (i < q.kc) fetch(code[i], i);
-            for (int c0 = 0; c0 < q.kc && ok; c0 += kAhead) {
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) {
-                    const int c = c0 + i;
-                    if (c >= q.kc) break;
-                    if (!tc::wait_bar_warp(bar_empty + 8 * st, ph ^ 1u, flags)) { ok = false; break; }
-                    uint8_t *dst = smem + st * kStage + kHalfStage;
-                    if (mine) {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            invalid |= (code[i][j] >> 1) & ~code[i][j] & 0x55555555u;
-                            *reinterpret_cast<uint4 *>(dst + tc::swz_offset((uint32_t)row, (uint32_t)(half * 4 + j), 128u)) = expand_16(code[i][j]);
-                        }
+                    for (int j = 0; j < 4; ++j) {
+                        invalid |= (code[i][j] >> 1) & ~code[i][j] & 0x55555555u;
+                        wide[i][j] = expand_16(code[i][j]);
                     }
-                    if (c + kAhead < q.kc) fetch(code[i], c + kAhead);
-                    publish(1);
-                }
+                if (c + kFillGroups < q.kc) fetch(c + kFillGroups);
+                if (!enter(n)) { ok = false; break; }
+                uint8_t *dst = smem + (n % kStages) * kStage + kHalfStage;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (row0 + 32 * i < rows) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            *reinterpret_cast<uint4 *>(dst + tc::swz_offset((uint32_t)(row0 + 32 * i), (uint32_t)(half * 4 + j), 128u)) = wide[i][j];
+                    }
+                publish(n, 1);
             }
+            seq += (uint32_t)q.kc;
             if (!ok || !p.a) continue;
             if (!waited) { ptx::grid_dep_wait(); waited = true; }
-            const int adapters = adapters_of_tile(mt);
-            const long long r = (long long)mt * kTile + (int)rank * 128 + row;
-            int mine_a = -1;
-            const float *t = p.t;
-            float power = 1.0f;
-            if (adapters && r < p.m) {
-                mine_a = __ldg(p.which + r / p.rows_per_sample);
-                if (mine_a < 0 || mine_a >= p.n) mine_a = -1;
-                if (mine_a >= 0) { t = p.t + r * pitch; power = 1.0f / row_power(t, pitch); }
-            }
-            for (int i = 0; i < adapters && ok; ++i) {
-                const int a = __ldcg(p.list + (size_t)mt * kListInts + 1 + i);
-                const H *b = static_cast<const H *>(p.b) + ((size_t)a * p.cout + (there ? o : 0)) * p.rank;
-                for (int c = 0; c < per_adapter; ++c) {
-                    if (!tc::wait_bar_warp(bar_empty + 8 * st, ph ^ 1u, flags)) { ok = false; break; }
-                    uint8_t *dst = smem + st * kStage;
-#pragma unroll 1
-                    for (int k = 0; k < 4; ++k) {
-                        const int e = c * 64 + half * 32 + 8 * k, term = e / pitch, j = e - term * pitch;     // (pitch is a multiple of 16)
-                        const uint32_t off = tc::swz_offset((uint32_t)row, (uint32_t)(half * 4 + k), 128u);
-                        uint4 av = make_uint4(0u, 0u, 0u, 0u), bv = av;
-                        if (e < k2 && mine_a == a) {
-                            const float4 t0 = *reinterpret_cast<const float4 *>(t + j), t1 = *reinterpret_cast<const float4 *>(t + j + 4);
-                            float v[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
+            const int chunks = adapters_of_tile(mt) * per_adapter;
+            int mine[4];                        // the rows' adapters
 #pragma unroll
-                            for (int s = 0; s < 8; ++s) {
-                                v[s] *= power;
-                                for (int m = 0; m < term; ++m) v[s] -= norm::to_float(norm::from_float<H>(v[s]));
-                            }
-                            av = make_uint4(pack_pair<H>(v[0], v[1]), pack_pair<H>(v[2], v[3]), pack_pair<H>(v[4], v[5]), pack_pair<H>(v[6], v[7]));
-                        }
+            for (int i = 0; i < 4; ++i) {
+                const long long r = (long long)mt * kTile + (int)rank * 128 + row0 + 32 * i;
+                mine[i] = chunks && r < p.m ? __ldg(p.which + r / p.rows_per_sample) : -1;
+            }
+            for (c = (int)(((uint32_t)grp - seq) % kFillGroups); c < chunks; c += kFillGroups) {
+                const uint32_t n = seq + (uint32_t)c;
+                const int i_ad = c / per_adapter, part = c - i_ad * per_adapter;
+                const int a = __ldcg(p.list + (size_t)mt * kListInts + 1 + i_ad);
+                if (!enter(n)) { ok = false; break; }
+                uint8_t *dst = smem + (n % kStages) * kStage;
+#pragma unroll 2
+                for (int i = 0; i < 4; ++i) {
+                    const int row = row0 + 32 * i;
+                    const long long r = (long long)mt * kTile + (int)rank * 128 + row;
+                    const bool there = row < rows && o0 + row < p.cout;
+                    const H *t16 = static_cast<const H *>(p.t16) + (size_t)r * k2;
+                    const H *b = static_cast<const H *>(p.b) + ((size_t)a * p.cout + (there ? o0 + row : 0)) * p.rank;
+                    uint4 av[4], bv[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int e = part * 64 + half * 32 + 8 * k, j = e - (e >= p.pitch ? p.pitch : 0) - (e >= 2 * p.pitch ? p.pitch : 0);
+                        av[k] = bv[k] = make_uint4(0u, 0u, 0u, 0u);
+                        if (e < k2 && mine[i] == a) av[k] = __ldcg(reinterpret_cast<const uint4 *>(t16 + e));
                         if (e < k2 && there && j < p.rank) {
-                            uint32_t w[4] = {0u, 0u, 0u, 0u};
                             if ((p.rank & 7) == 0) {
-                                const uint4 v = __ldg(reinterpret_cast<const uint4 *>(b + j));
-                                w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+                                bv[k] = __ldg(reinterpret_cast<const uint4 *>(b + j));
                             } else {
+                                uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
                                 for (int s = 0; s < 8; ++s)
                                     if (j + s < p.rank) w[s >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short *>(b) + j + s) << (16 * (s & 1));
+                                bv[k] = make_uint4(w[0], w[1], w[2], w[3]);
                             }
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t off = tc::swz_offset((uint32_t)row, (uint32_t)(half * 4 + k), 128u);
+                        *reinterpret_cast<uint4 *>(dst + off) = av[k];
+                        if (row < rows) {
+                            uint32_t w[4] = {bv[k].x, bv[k].y, bv[k].z, bv[k].w};
                             constexpr uint32_t top = std::is_same<H, __nv_bfloat16>::value ? 0x7F80u : 0x7C00u;    // the exponent of what is not finite
 #pragma unroll
                             for (int s = 0; s < 4; ++s) {
                                 if ((w[s] & top) == top) { w[s] &= 0xFFFF0000u; bad = true; }
                                 if (((w[s] >> 16) & top) == top) { w[s] &= 0x0000FFFFu; bad = true; }
                             }
-                            bv = make_uint4(w[0], w[1], w[2], w[3]);
+                            *reinterpret_cast<uint4 *>(dst + kHalfStage + off) = make_uint4(w[0], w[1], w[2], w[3]);
                         }
-                        *reinterpret_cast<uint4 *>(dst + off) = av;
-                        if (mine) *reinterpret_cast<uint4 *>(dst + kHalfStage + off) = bv;
                     }
-                    publish(warp == kFill0 && rank == 0 ? 2u : 1u);     // (the loader's arrival among them)
                 }
+                publish(n, ft < 32 && rank == 0 ? 2u : 1u);     // (the loader's arrival among them)
             }
+            seq += (uint32_t)chunks;
         }
         if (invalid || bad) raise_status(PROM_ERR_BAD_WEIGHT);
         __syncwarp();
@@ -762,7 +816,7 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                 if (adapters) {
                     const int a = __ldg(p.which + s);
                     with = a >= 0 && a < p.n;
-                    if (with) ad = (p.scale ? __ldg(p.scale + a) : 1.0f) * fac * row_power(p.t + r * pitch, pitch);
+                    if (with) ad = (p.scale ? __ldg(p.scale + a) : 1.0f) * fac * __ldcg(p.power + r);
                 }
             }
             if (!tc::wait_bar<true>(bar_tfull, done & 1u, flags)) break;

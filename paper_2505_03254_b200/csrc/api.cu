@@ -2415,10 +2415,12 @@ static int tile_pairs(const DeviceInfo &d)
 
 static long long row_tiles(long long m) { return (m + kTile - 1) / kTile; }
 static int pitch_of(int rank) { return (rank + 15) & ~15; }
-static size_t t_bytes(long long m, int rank) { return round256((size_t)m * pitch_of(rank) * sizeof(float)); }
+// The workspace of many rows: the 16-bit values (room for three of each), the rows' powers, the tiles' lists.  It covers
+// the inner products of few rows too.
+static size_t t16_bytes(long long m, int rank) { return round256((size_t)m * pitch_of(rank) * 3 * 2); }
 static size_t workspace_bytes(long long m, int rank)
 {
-    return t_bytes(m, rank) + round256((size_t)row_tiles(m) * kListInts * sizeof(int));
+    return t16_bytes(m, rank) + round256((size_t)m * sizeof(float)) + round256((size_t)row_tiles(m) * kListInts * sizeof(int));
 }
 
 template <class H, class Y>
@@ -2435,7 +2437,6 @@ static prom_status run_tiles(Params &p, int y_type, const DeviceInfo &d, cudaStr
     q.nt = 256;
     while (q.nt > 64 && (long long)q.n_mtiles * ((p.cout + q.nt - 1) / q.nt) < pairs) q.nt /= 2;
     q.n_ctiles = (p.cout + q.nt - 1) / q.nt;
-    q.terms = y_type == PROM_TYPE_F32 ? 3 : 2;
     const size_t bytes = norm::type_bytes(y_type);
     q.store = norm::whole_pieces(p.y, p.y_pitch, bytes);
     CUtensorMap xmap, ymap;
@@ -2467,15 +2468,18 @@ static prom_status run_tiles(Params &p, int y_type, const DeviceInfo &d, cudaStr
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];
     if (p.a) {
-        p.t_pitch = pitch_of(p.rank);
-        p.list = reinterpret_cast<int *>(reinterpret_cast<uint8_t *>(p.t) + t_bytes(p.m, p.rank));
-        if (raise_smem_limit(inner_tiles_kernel<H>, kInnerSmem) != cudaSuccess) return PROM_ERR_CUDA;
-        fill_launch_cfg(cfg, attr, 1, 32 * kInnerWarps, kInnerSmem, st, true);
-        // a tile's items over several blocks: four of a run of 256 rows, more where there are few tiles
-        const int zs = (p.t_pitch + 31) / 32;
-        long long share = (2ll * d.sms + (long long)q.n_mtiles * zs - 1) / ((long long)q.n_mtiles * zs);
-        share = share < 4 ? 4 : (share > 32 ? 32 : share);
-        cfg.gridDim = dim3((unsigned)q.n_mtiles, (unsigned)share, (unsigned)zs);
+        p.pitch = pitch_of(p.rank);
+        p.terms = y_type == PROM_TYPE_F32 ? 3 : 2;
+        uint8_t *ws = reinterpret_cast<uint8_t *>(p.t);
+        p.t16 = ws;
+        p.power = reinterpret_cast<float *>(ws + t16_bytes(p.m, p.rank));
+        p.list = reinterpret_cast<int *>(ws + t16_bytes(p.m, p.rank) + round256((size_t)p.m * sizeof(float)));
+        if (raise_smem_limit(inner_tiles_kernel<H>, (int)inner_smem(kMaxRank)) != cudaSuccess) return PROM_ERR_CUDA;
+        fill_launch_cfg(cfg, attr, 1, 32 * kInnerWarps, inner_smem(p.pitch), st, true);
+        // a tile's items over several blocks: eight of a run of 256 rows, more where there are few tiles
+        long long share = (2ll * d.sms + q.n_mtiles - 1) / q.n_mtiles;
+        share = share < 8 ? 8 : (share > 32 ? 32 : share);
+        cfg.gridDim = dim3((unsigned)q.n_mtiles, (unsigned)share);
         const cudaError_t e = cudaLaunchKernelEx(&cfg, inner_tiles_kernel<H>, p);
         ++g_launches;
         if (e != cudaSuccess) return cuda_status(e);
@@ -2494,7 +2498,6 @@ static prom_status run_as(Params &p, int y_type, const DeviceInfo &d, cudaStream
 {
     const int mode = g_adapters_mode.load();
     if (mode == 2 || (mode == 0 && p.m > 128)) return run_tiles<H, Y>(p, y_type, d, st);
-    p.t_pitch = p.rank;
     return run_rows<H, Y>(p, st);
 }
 

@@ -90,7 +90,8 @@ SHAPES = [  # batch, rows, cin, cout, adapters, rank
     (32, 1, 1024, 512, 40, 16), (33, 1, 320, 104, 5, 12), (64, 1, 256, 384, 64, 32), (100, 1, 144, 200, 7, 64), (127, 1, 400, 8, 3, 5),
     (128, 1, 1536, 128, 16, 24), (129, 1, 208, 264, 4, 48), (205, 1, 960, 1280, 5, 8), (256, 1, 512, 640, 3, 100), (257, 1, 64, 520, 2, 256),
     (300, 1, 384, 1032, 300, 8), (600, 1, 2048, 256, 30, 16), (1000, 1, 16, 72, 12, 3), (5, 49, 576, 160, 3, 4), (4, 196, 384, 576, 12, 4),
-    (2, 700, 96, 24, 1, 64), (1024, 1, 4096, 512, 16, 64), (2500, 1, 128, 256, 9, 16), (40, 64, 160, 960, 6, 31)]
+    (2, 700, 96, 24, 1, 64), (1024, 1, 4096, 512, 16, 64), (2500, 1, 128, 256, 9, 16), (1100, 1, 256, 1024, 60, 16), (5000, 1, 48, 1280, 200, 8),
+    (9000, 1, 512, 264, 2, 40), (40, 64, 160, 960, 6, 31)]
 
 
 @pytest.mark.parametrize("shape", SHAPES)

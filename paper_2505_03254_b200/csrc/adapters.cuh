@@ -27,10 +27,11 @@ struct Params {
     long long y_pitch;
     float *t;                       // [m][rank] inner products (few rows)
     // Many rows: the inner products as sums of `terms` 16-bit values, [m][terms][pitch] (pitch: rank rounded up to 16, zeros
-    // behind it), divided by a power of two per row; and per tile of 256 rows the number of its adapters and these.
+    // behind it), divided by a power of two per row; the rows' adapters; and per tile of 256 rows the number of its adapters
+    // and these.
     void *t16;
     float *power;
-    int *list;
+    int *list, *row_adapter;
     int pitch, terms;
     int chained;                    // a kernel of the same call is in front: only what that one writes is waited for
 };
@@ -251,17 +252,20 @@ proj_rows_kernel(const Params p)
 }
 
 // ---- many rows: inner products ----------------------------------------------------------------------------------
-// Rows in tiles of 256.  A block sorts the tile's rows by their adapter (each thread counts the rows that come before its
-// own), so that any order of requests costs what runs of requests cost: an item is up to 32 rows of one adapter, found
-// by index, and the items go round the blocks of a tile.  The eight warps share K and multiply with the warp-level
-// 16-bit MMA, rows as A (int8 values are exact in both 16-bit types) and the adapter as B; a thread's 16 bytes of a row and
-// 32 of the adapter are 16 neighbouring values of k, whose order inside the MMAs is free.  The sums are then split into
-// 16-bit values once, for all the projection's tiles of outputs.
+// Rows in tiles of 256.  A block sorts the tile's rows by their adapter (a row's place is the number of smaller keys), so
+// that any order of requests costs what runs of requests cost: an item is up to 32 rows of one adapter, and the items go
+// round the blocks of a tile.  K comes through shared memory in stages of 256; each of the eight warps multiplies its 32
+// of them with the warp-level 16-bit MMA, rows as A (int8 values are exact in both 16-bit types) and the adapter as B, and
+// the warps' sums are added at the end.  A thread's 8 bytes of a row and 16 of the adapter are 8 neighbouring values of k, whose
+// order inside the MMAs is free.  The sums are then split into 16-bit values once, for all the projection's tiles of outputs.
 constexpr int kTile = 256;
 constexpr int kItemRows = 32;
 constexpr int kListInts = kTile + 1;
 constexpr int kInnerWarps = 8;
 constexpr int kRankPart = 64;               // ranks of one pass over K
+constexpr int kInnerK = 32 * kInnerWarps;   // values of k per stage
+constexpr uint32_t kXPitch = kInnerK + 32, kAPitch = 2 * kInnerK + 64;      // bytes: a warp's accesses fall into different banks
+constexpr int kInnerStages = 2;
 
 // Four int8 values (one word) to two words of 16-bit values: 0, 1 and 2, 3.
 template <class H> __device__ __forceinline__ void widen_4(uint32_t w, uint32_t &lo, uint32_t &hi);
@@ -318,19 +322,26 @@ __device__ __forceinline__ float row_power(float top)
     return e <= 14u || e == 255u ? 1.0f : __uint_as_float((e - 13u) << 23);
 }
 
-// Shared memory: partial sums [warp][row][kRankPart + 1], then the item's sums [row][pitch].
+// Shared memory: the stages (rows, then ranks), afterwards the warps' sums [warp][row][kPartPitch]; behind them the item's
+// sums [row][pitch].
 constexpr int kPartPitch = kRankPart + 1;
-constexpr int kPartFloats = kInnerWarps * kItemRows * kPartPitch;
-static inline size_t inner_smem(int pitch) { return (size_t)(kPartFloats + kItemRows * pitch) * sizeof(float); }
+static __host__ __device__ inline uint32_t inner_stage(int pitch) { return kItemRows * kXPitch + (uint32_t)(pitch < kRankPart ? pitch : kRankPart) * kAPitch; }
+static __host__ __device__ inline uint32_t inner_sums_at(int pitch)
+{
+    const uint32_t a = kInnerStages * inner_stage(pitch), b = kInnerWarps * kItemRows * kPartPitch * 4u;
+    return a > b ? a : b;
+}
+static inline size_t inner_smem(int pitch) { return inner_sums_at(pitch) + (size_t)kItemRows * pitch * sizeof(float); }
 
 template <class H>
-__global__ void __launch_bounds__(32 * kInnerWarps)
+__global__ void __launch_bounds__(32 * kInnerWarps, 2)
 inner_tiles_kernel(const Params p)
 {
-    extern __shared__ float part[];
-    float *sums = part + kPartFloats;
+    extern __shared__ __align__(16) uint8_t smem[];
+    float *part = reinterpret_cast<float *>(smem), *sums = reinterpret_cast<float *>(smem + inner_sums_at(p.pitch));
     __shared__ __align__(16) int key_s[kTile];
-    __shared__ int row_s[kTile];                // rows in the order of their adapters
+    __shared__ int sorted_s[kTile + 1];         // adapter << 8 | row
+    __shared__ unsigned start_s[kTile / 32];    // places where another adapter begins
     __shared__ int item_s[kTile];               // first place | rows << 16
     __shared__ int warp_items[kTile / 32], warp_lists[kTile / 32];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -338,26 +349,37 @@ inner_tiles_kernel(const Params p)
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
 
-    // places: rows without an adapter have none
-    const int key = first + tid < p.m ? adapter_of(p, (first + tid) / p.rows_per_sample) : -1;
+    // rows without an adapter come last (adapters are below 2^20)
+    constexpr int kNone = 1 << 20;
+    const int mine = first + tid < p.m ? adapter_of(p, (first + tid) / p.rows_per_sample) : -1;
+    const int key = (mine < 0 ? kNone : mine) << 8 | tid;
     key_s[tid] = key;
+    if (blockIdx.y == 0 && first + tid < p.m) p.row_adapter[first + tid] = mine;
     __syncthreads();
-    int less = 0, same_before = 0, same = 0;
-#pragma unroll 4
+    int place = 0;
+#pragma unroll 8
     for (int i = 0; i < kTile; i += 4) {
-        const int4 k4 = *reinterpret_cast<const int4 *>(key_s + i);
-        const int k[4] = {k4.x, k4.y, k4.z, k4.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            less += k[e] >= 0 && k[e] < key;
-            same += k[e] == key;
-            same_before += k[e] == key && i + e < tid;
-        }
+        const int4 k = *reinterpret_cast<const int4 *>(key_s + i);
+        place += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
     }
-    const int place = less + same_before;
-    if (key >= 0) row_s[place] = tid;
-    // an item starts at every 32nd row of an adapter; the list of adapters has their first rows
-    const bool head = key >= 0 && same_before % kItemRows == 0, newcomer = key >= 0 && same_before == 0;
+    sorted_s[place] = key;
+    if (tid == 0) sorted_s[kTile] = -1;         // (an adapter that no row has)
+    __syncthreads();
+    // from here on a thread is a place
+    const int a_here = sorted_s[tid] >> 8;
+    const bool start = tid == 0 || (sorted_s[tid - 1] >> 8) != a_here;
+    const unsigned starts = __ballot_sync(0xFFFFFFFFu, start);
+    if (lane == 0) start_s[warp] = starts;
+    __syncthreads();
+    const unsigned upto = 0xFFFFFFFFu >> (31 - lane), below = upto >> 1;
+    int begin;                                  // of this place's adapter
+    {
+        int w = warp;
+        unsigned mask = starts & upto;
+        while (!mask) mask = start_s[--w];      // (place 0 is a start)
+        begin = 32 * w + 31 - __clz(mask);
+    }
+    const bool real = a_here != kNone, head = real && (tid - begin) % kItemRows == 0, newcomer = real && start;
     const unsigned heads = __ballot_sync(0xFFFFFFFFu, head), news = __ballot_sync(0xFFFFFFFFu, newcomer);
     if (lane == 0) { warp_items[warp] = __popc(heads); warp_lists[warp] = __popc(news); }
     __syncthreads();
@@ -367,32 +389,44 @@ inner_tiles_kernel(const Params p)
         items += warp_items[w];
         adapters += warp_lists[w];
     }
-    const unsigned below = (1u << lane) - 1u;
     if (head) {
-        const int left = same - same_before;
-        item_s[before + __popc(heads & below)] = place | ((left < kItemRows ? left : kItemRows) << 16);
+        int n = 1;
+        while (n < kItemRows && (sorted_s[tid + n] >> 8) == a_here) ++n;
+        item_s[before + __popc(heads & below)] = tid | (n << 16);
     }
     if (blockIdx.y == 0) {
         int *list = p.list + tile * kListInts;
-        if (newcomer) list[1 + list_before + __popc(news & below)] = key;
+        if (newcomer) list[1 + list_before + __popc(news & below)] = a_here;
         if (tid == 0) list[0] = adapters;
     }
     __syncthreads();
 
+    const uint32_t base = ptx::smem_u32(smem), stage_bytes = inner_stage(p.pitch);
+    const int steps = (p.cin + kInnerK - 1) / kInnerK;
     for (int it = blockIdx.y; it < items; it += gridDim.y) {
         const int at = item_s[it] & 0xFFFF, count = item_s[it] >> 16;
-        const int a = key_s[row_s[at]];
+        const int a = sorted_s[at] >> 8;
         const H *am = static_cast<const H *>(p.a) + (size_t)a * p.rank * p.cin;
-        const int8_t *xr[2][2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int k = 16 * i + 8 * h + g;
-                xr[i][h] = p.x + (first + row_s[at + (k < count ? k : 0)]) * p.cin;
-            }
         for (int j0 = 0; j0 < p.pitch; j0 += kRankPart) {
             const int ranks = p.pitch - j0 < kRankPart ? p.pitch - j0 : kRankPart;      // a multiple of 16
+            // 16-byte pieces: a row has kInnerK / 16 of them, a rank kInnerK / 8; zeros past cin and rank
+            auto fetch = [&](int step) {
+                const uint32_t dst = base + (uint32_t)(step % kInnerStages) * stage_bytes;
+                const int k0 = step * kInnerK;
+                for (int i = tid; i < kItemRows * (kInnerK / 16); i += 32 * kInnerWarps) {
+                    const int row = i / (kInnerK / 16), piece = i % (kInnerK / 16), k = k0 + 16 * piece;
+                    const bool there = row < count && k < p.cin;
+                    const int8_t *src = p.x + (first + (sorted_s[at + (row < count ? row : 0)] & 255)) * p.cin + (there ? k : 0);
+                    ptx::cp_async_16_or_zero(dst + (uint32_t)row * kXPitch + 16u * piece, src, there);
+                }
+                for (int i = tid; i < ranks * (kInnerK / 8); i += 32 * kInnerWarps) {
+                    const int row = i / (kInnerK / 8), piece = i % (kInnerK / 8), k = k0 + 8 * piece;
+                    const bool there = j0 + row < p.rank && k < p.cin;
+                    ptx::cp_async_16_or_zero(dst + kItemRows * kXPitch + (uint32_t)row * kAPitch + 16u * piece,
+                                             am + (there ? (size_t)(j0 + row) * p.cin + k : 0), there);
+                }
+                ptx::cp_async_commit();
+            };
             float acc[2][8][4];                 // [16 rows][8 ranks][...]
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -400,58 +434,44 @@ inner_tiles_kernel(const Params p)
                 for (int j = 0; j < 8; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
-            for (int k = warp * 64 + 16 * t; k < ((p.cin + 63) & ~63); k += 64 * kInnerWarps) {
-                const bool in = k < p.cin;
-                uint32_t xw[2][2][4];
+            fetch(0);
+            for (int step = 0; step < steps; ++step) {
+                if (step + 1 < steps) { fetch(step + 1); ptx::cp_async_wait<1>(); }
+                else ptx::cp_async_wait<0>();
+                __syncthreads();
+                const uint8_t *sx = smem + (uint32_t)(step % kInnerStages) * stage_bytes + 32 * warp + 8 * t;
+                const uint8_t *sa = smem + (uint32_t)(step % kInnerStages) * stage_bytes + kItemRows * kXPitch + 64 * warp + 16 * t;
+                uint32_t f[2][2][4];            // [16 rows][first, second 16 of k]
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                        if (in && 16 * i < count) v = __ldg(reinterpret_cast<const uint4 *>(xr[i][h] + k));
-                        xw[i][h][0] = v.x; xw[i][h][1] = v.y; xw[i][h][2] = v.z; xw[i][h][3] = v.w;
-                    }
-#pragma unroll
-                for (int jj = 0; jj < 8; jj += 4) {
-                    if (8 * jj >= ranks) break;
-                    uint32_t b[4][8];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int rk = j0 + 8 * (jj + j) + g;
-                        uint4 v0 = make_uint4(0u, 0u, 0u, 0u), v1 = v0;
-                        if (in && rk < p.rank) {
-                            const uint4 *src = reinterpret_cast<const uint4 *>(am + (size_t)rk * p.cin + k);
-                            v0 = __ldg(src); v1 = __ldg(src + 1);
-                        }
-                        b[j][0] = v0.x; b[j][1] = v0.y; b[j][2] = v0.z; b[j][3] = v0.w;
-                        b[j][4] = v1.x; b[j][5] = v1.y; b[j][6] = v1.z; b[j][7] = v1.w;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        if (16 * i >= count) break;
-#pragma unroll
-                        for (int s = 0; s < 4; ++s) {
-                            uint32_t f[4];
-                            widen_4<H>(xw[i][0][s], f[0], f[2]);
-                            widen_4<H>(xw[i][1][s], f[1], f[3]);
-#pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                if (8 * (jj + j) < ranks) mma_16<H>(acc[i][jj + j], f, b[j][2 * s], b[j][2 * s + 1]);
-                        }
-                    }
+                for (int i = 0; i < 2; ++i) {
+                    const uint2 lo = *reinterpret_cast<const uint2 *>(sx + (uint32_t)(16 * i + g) * kXPitch);
+                    const uint2 hi = *reinterpret_cast<const uint2 *>(sx + (uint32_t)(16 * i + 8 + g) * kXPitch);
+                    widen_4<H>(lo.x, f[i][0][0], f[i][0][2]);
+                    widen_4<H>(hi.x, f[i][0][1], f[i][0][3]);
+                    widen_4<H>(lo.y, f[i][1][0], f[i][1][2]);
+                    widen_4<H>(hi.y, f[i][1][1], f[i][1][3]);
                 }
-            }
-            float *mine = part + (size_t)warp * kItemRows * kPartPitch;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (16 * i >= count) break;
+                for (int j = 0; j < 8; ++j)
+                    if (8 * j < ranks) {
+                        const uint4 b = *reinterpret_cast<const uint4 *>(sa + (uint32_t)(8 * j + g) * kAPitch);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            mma_16<H>(acc[i][j], f[i][0], b.x, b.y);
+                            mma_16<H>(acc[i][j], f[i][1], b.z, b.w);
+                        }
+                    }
+                __syncthreads();                // the stage may be filled again
+            }
+            float *own = part + (size_t)warp * kItemRows * kPartPitch;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
                     if (8 * j < ranks) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) mine[(16 * i + g + 8 * (e >> 1)) * kPartPitch + 8 * j + 2 * t + (e & 1)] = acc[i][j][e];
+                        for (int e = 0; e < 4; ++e) own[(16 * i + g + 8 * (e >> 1)) * kPartPitch + 8 * j + 2 * t + (e & 1)] = acc[i][j][e];
                     }
-            }
             __syncthreads();
             for (int i = tid; i < count * ranks; i += 32 * kInnerWarps) {
                 const int k = i / ranks, j = i - k * ranks;
@@ -468,7 +488,7 @@ inner_tiles_kernel(const Params p)
             float top = 0.0f;
             for (int j = lane; j < p.pitch; j += 32) top = norm::max_nan(top, fabsf(v[j]));
             const float power = row_power(norm::warp_max(top)), by = 1.0f / power;
-            const long long r = first + row_s[at + k];
+            const long long r = first + (sorted_s[at + k] & 255);
             if (lane == 0) p.power[r] = power;
             uint32_t *out = static_cast<uint32_t *>(p.t16) + (size_t)r * p.terms * (p.pitch / 2);
             for (int j = lane; j < p.pitch / 2; j += 32) {
@@ -496,7 +516,7 @@ inner_tiles_kernel(const Params p)
 constexpr int kFillGroups = 4, kGroupWarps = 2, kFillWarps = kFillGroups * kGroupWarps, kEpiWarps = 8;
 constexpr int kFill0 = 2, kEpi0 = kFill0 + kFillWarps;
 constexpr int kTileThreads = 32 * (kEpi0 + kEpiWarps);
-constexpr int kStages = 6;
+constexpr int kStages = 4;
 constexpr uint32_t kHalfStage = 128u * 128u, kStage = 2u * kHalfStage;      // rows of x, rows of weights: 128 bytes of K each
 constexpr uint32_t kSlab = 32u * 128u;                                      // an epilogue warp's 32 rows x 32 outputs
 constexpr uint32_t kOffSlab = kStages * kStage;
@@ -705,6 +725,20 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                     }
                 }
             };
+            // the tile's adapters and the rows' own, looked up a whole pass over K before they are needed
+            const int *list = p.list + (size_t)mt * kListInts;
+            int chunks = 0, mine[4], held[2];
+            auto look = [&] {
+                chunks = __ldcg(list) * per_adapter;
+                held[0] = __ldcg(list + 1);         // (what lies past the number is not used)
+                held[1] = __ldcg(list + 2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const long long r = (long long)mt * kTile + (int)rank * 128 + row0 + 32 * i;
+                    mine[i] = r < p.m ? __ldcg(p.row_adapter + r) : -1;
+                }
+            };
+            if (p.a && waited) look();
             int c = (int)(((uint32_t)grp - seq) % kFillGroups);
             if (c < q.kc) fetch(c);
             for (; c < q.kc; c += kFillGroups) {
@@ -732,61 +766,57 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
             }
             seq += (uint32_t)q.kc;
             if (!ok || !p.a) continue;
-            if (!waited) { ptx::grid_dep_wait(); waited = true; }
-            const int chunks = adapters_of_tile(mt) * per_adapter;
-            int mine[4];                        // the rows' adapters
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const long long r = (long long)mt * kTile + (int)rank * 128 + row0 + 32 * i;
-                mine[i] = chunks && r < p.m ? __ldg(p.which + r / p.rows_per_sample) : -1;
-            }
+            if (!waited) { ptx::grid_dep_wait(); waited = true; look(); }
             for (c = (int)(((uint32_t)grp - seq) % kFillGroups); c < chunks; c += kFillGroups) {
                 const uint32_t n = seq + (uint32_t)c;
                 const int i_ad = c / per_adapter, part = c - i_ad * per_adapter;
-                const int a = __ldcg(p.list + (size_t)mt * kListInts + 1 + i_ad);
+                const int a = i_ad == 0 ? held[0] : (i_ad == 1 ? held[1] : __ldcg(list + 1 + i_ad));
+                const int e0 = part * 64 + half * 32;
                 if (!enter(n)) { ok = false; break; }
-                uint8_t *dst = smem + (n % kStages) * kStage;
-#pragma unroll 2
+                const uint32_t dst = base + (n % kStages) * kStage;
+                const bool wide_b = (p.rank & 7) == 0;
+#pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int row = row0 + 32 * i;
                     const long long r = (long long)mt * kTile + (int)rank * 128 + row;
                     const bool there = row < rows && o0 + row < p.cout;
-                    const H *t16 = static_cast<const H *>(p.t16) + (size_t)r * k2;
+                    const H *t16 = static_cast<const H *>(p.t16) + (size_t)(mine[i] == a ? r : 0) * k2;
                     const H *b = static_cast<const H *>(p.b) + ((size_t)a * p.cout + (there ? o0 + row : 0)) * p.rank;
-                    uint4 av[4], bv[4];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const int e = part * 64 + half * 32 + 8 * k, j = e - (e >= p.pitch ? p.pitch : 0) - (e >= 2 * p.pitch ? p.pitch : 0);
-                        av[k] = bv[k] = make_uint4(0u, 0u, 0u, 0u);
-                        if (e < k2 && mine[i] == a) av[k] = __ldcg(reinterpret_cast<const uint4 *>(t16 + e));
-                        if (e < k2 && there && j < p.rank) {
-                            if ((p.rank & 7) == 0) {
-                                bv[k] = __ldg(reinterpret_cast<const uint4 *>(b + j));
-                            } else {
-                                uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-                                for (int s = 0; s < 8; ++s)
-                                    if (j + s < p.rank) w[s >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short *>(b) + j + s) << (16 * (s & 1));
-                                bv[k] = make_uint4(w[0], w[1], w[2], w[3]);
-                            }
-                        }
-                    }
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
+                        const int e = e0 + 8 * k, j = e - (e >= p.pitch ? p.pitch : 0) - (e >= 2 * p.pitch ? p.pitch : 0);
                         const uint32_t off = tc::swz_offset((uint32_t)row, (uint32_t)(half * 4 + k), 128u);
-                        *reinterpret_cast<uint4 *>(dst + off) = av[k];
-                        if (row < rows) {
-                            uint32_t w[4] = {bv[k].x, bv[k].y, bv[k].z, bv[k].w};
-                            constexpr uint32_t top = std::is_same<H, __nv_bfloat16>::value ? 0x7F80u : 0x7C00u;    // the exponent of what is not finite
+                        const bool t_in = e < k2 && mine[i] == a, b_in = e < k2 && there && j < p.rank;
+                        ptx::cp_async_16_or_zero(dst + off, t16 + (t_in ? e : 0), t_in);
+                        if (wide_b) {
+                            ptx::cp_async_16_or_zero(dst + kHalfStage + off, b + (b_in ? j : 0), b_in);
+                        } else {
+                            uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-                            for (int s = 0; s < 4; ++s) {
-                                if ((w[s] & top) == top) { w[s] &= 0xFFFF0000u; bad = true; }
-                                if (((w[s] >> 16) & top) == top) { w[s] &= 0x0000FFFFu; bad = true; }
-                            }
-                            *reinterpret_cast<uint4 *>(dst + kHalfStage + off) = make_uint4(w[0], w[1], w[2], w[3]);
+                            for (int s = 0; s < 8; ++s)
+                                if (b_in && j + s < p.rank) w[s >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short *>(b) + j + s) << (16 * (s & 1));
+                            ptx::sts_128(dst + kHalfStage + off, w[0], w[1], w[2], w[3]);
                         }
                     }
                 }
+                ptx::cp_async_wait_all();
+                // what is not finite in B counts as zero
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t at = dst + kHalfStage + tc::swz_offset((uint32_t)(row0 + 32 * i), (uint32_t)(half * 4 + k), 128u);
+                        const int4 v = ptx::lds_128(at);
+                        uint32_t w[4] = {(uint32_t)v.x, (uint32_t)v.y, (uint32_t)v.z, (uint32_t)v.w};
+                        constexpr uint32_t top = std::is_same<H, __nv_bfloat16>::value ? 0x7F80u : 0x7C00u;    // its exponent
+                        bool hit = false;
+#pragma unroll
+                        for (int s = 0; s < 4; ++s) {
+                            if ((w[s] & top) == top) { w[s] &= 0xFFFF0000u; hit = true; }
+                            if (((w[s] >> 16) & top) == top) { w[s] &= 0x0000FFFFu; hit = true; }
+                        }
+                        if (hit) { bad = true; ptx::sts_128(at, w[0], w[1], w[2], w[3]); }
+                    }
                 publish(n, ft < 32 && rank == 0 ? 2u : 1u);     // (the loader's arrival among them)
             }
             seq += (uint32_t)chunks;
@@ -814,8 +844,8 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                 const long long s = r / p.rows_per_sample;
                 fac = row_factor(p, s);
                 if (adapters) {
-                    const int a = __ldg(p.which + s);
-                    with = a >= 0 && a < p.n;
+                    const int a = __ldcg(p.row_adapter + r);
+                    with = a >= 0;
                     if (with) ad = (p.scale ? __ldg(p.scale + a) : 1.0f) * fac * __ldcg(p.power + r);
                 }
             }

@@ -2415,12 +2415,12 @@ static int tile_pairs(const DeviceInfo &d)
 
 static long long row_tiles(long long m) { return (m + kTile - 1) / kTile; }
 static int pitch_of(int rank) { return (rank + 15) & ~15; }
-// The workspace of many rows: the 16-bit values (room for three of each), the rows' powers, the tiles' lists.  It covers
-// the inner products of few rows too.
+// The workspace of many rows: the 16-bit values (room for three of each), the rows' powers and adapters, the tiles'
+// lists.  It covers the inner products of few rows too.
 static size_t t16_bytes(long long m, int rank) { return round256((size_t)m * pitch_of(rank) * 3 * 2); }
 static size_t workspace_bytes(long long m, int rank)
 {
-    return t16_bytes(m, rank) + round256((size_t)m * sizeof(float)) + round256((size_t)row_tiles(m) * kListInts * sizeof(int));
+    return t16_bytes(m, rank) + 2 * round256((size_t)m * sizeof(float)) + round256((size_t)row_tiles(m) * kListInts * sizeof(int));
 }
 
 template <class H, class Y>
@@ -2473,7 +2473,8 @@ static prom_status run_tiles(Params &p, int y_type, const DeviceInfo &d, cudaStr
         uint8_t *ws = reinterpret_cast<uint8_t *>(p.t);
         p.t16 = ws;
         p.power = reinterpret_cast<float *>(ws + t16_bytes(p.m, p.rank));
-        p.list = reinterpret_cast<int *>(ws + t16_bytes(p.m, p.rank) + round256((size_t)p.m * sizeof(float)));
+        p.row_adapter = reinterpret_cast<int *>(ws + t16_bytes(p.m, p.rank) + round256((size_t)p.m * sizeof(float)));
+        p.list = reinterpret_cast<int *>(ws + t16_bytes(p.m, p.rank) + 2 * round256((size_t)p.m * sizeof(float)));
         if (raise_smem_limit(inner_tiles_kernel<H>, (int)inner_smem(kMaxRank)) != cudaSuccess) return PROM_ERR_CUDA;
         fill_launch_cfg(cfg, attr, 1, 32 * kInnerWarps, inner_smem(p.pitch), st, true);
         // a tile's items over several blocks: eight of a run of 256 rows, more where there are few tiles

@@ -36,14 +36,18 @@ struct Params {
     int chained;                    // a kernel of the same call is in front: only what that one writes is waited for
 };
 
-__device__ __forceinline__ float row_factor(const Params &p, long long s)
+__device__ __forceinline__ int sample_of(const Params &p, long long r)     // (both below 2^31)
+{
+    return p.rows_per_sample == 1 ? (int)r : (int)((uint32_t)r / (uint32_t)p.rows_per_sample);
+}
+__device__ __forceinline__ float row_factor(const Params &p, int s)
 {
     const float g = __ldg(p.gamma + s);
     return __fdiv_rn(g < 1e-5f ? 1e-5f : g, 127.0f);        // (a NaN stays one)
 }
 
 // The adapter of a sample, -1 for none.  An index that is outside the table counts as none and is reported.
-__device__ __forceinline__ int adapter_of(const Params &p, long long s)
+__device__ __forceinline__ int adapter_of(const Params &p, int s)
 {
     if (!p.a) return -1;
     const int a = __ldg(p.which + s);
@@ -73,7 +77,7 @@ inner_rows_kernel(const Params p)
     ptx::grid_dep_launch();
     const long long r = blockIdx.x;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = blockIdx.y * 8 + warp;
-    const int a = adapter_of(p, r / p.rows_per_sample);
+    const int a = adapter_of(p, sample_of(p, r));
     if (a < 0 || j >= p.rank) return;
     const uint4 *x = reinterpret_cast<const uint4 *>(p.x + r * p.cin);
     const uint4 *av = reinterpret_cast<const uint4 *>(static_cast<const H *>(p.a) + ((size_t)a * p.rank + j) * p.cin);
@@ -241,7 +245,7 @@ proj_rows_kernel(const Params p)
         int acc = 0;
 #pragma unroll
         for (int w = 0; w < kRowWarps; ++w) acc += acc_s[w][o][c] - 2 * sum_s[w][c];
-        const long long s = r / p.rows_per_sample;
+        const int s = sample_of(p, r);
         const float f = row_factor(p, s);
         float y = (float)acc * __ldg(p.alpha + o0 + o) * f;
         const int a = adapter_of(p, s);
@@ -254,18 +258,20 @@ proj_rows_kernel(const Params p)
 // ---- many rows: inner products ----------------------------------------------------------------------------------
 // Rows in tiles of 256.  A block sorts the tile's rows by their adapter (a row's place is the number of smaller keys), so
 // that any order of requests costs what runs of requests cost: an item is up to 32 rows of one adapter, and the items go
-// round the blocks of a tile.  K comes through shared memory in stages of 256; each of the eight warps multiplies its 32
-// of them with the warp-level 16-bit MMA, rows as A (int8 values are exact in both 16-bit types) and the adapter as B, and
-// the warps' sums are added at the end.  A thread's 8 bytes of a row and 16 of the adapter are 8 neighbouring values of k, whose
-// order inside the MMAs is free.  The sums are then split into 16-bit values once, for all the projection's tiles of outputs.
+// round the blocks of a tile.  K comes in stages of 256 by asynchronous copies of 16 bytes (a bulk copy per row and rank took
+// twice as long: they are a few hundred bytes each); each of the eight warps multiplies its 32 of them with the warp-level
+// 16-bit MMA, rows as A (int8 values are exact in both 16-bit types) and the adapter as B, and the warps' sums are added at
+// the end.  A thread's 8 bytes of a row and 16 of the adapter are 8 neighbouring values of k, whose order inside the MMAs
+// is free.  The sums are then split into 16-bit values once, for all the projection's tiles of outputs.
 constexpr int kTile = 256;
 constexpr int kItemRows = 32;
 constexpr int kListInts = kTile + 1;
 constexpr int kInnerWarps = 8;
 constexpr int kRankPart = 64;               // ranks of one pass over K
+constexpr int kInnerThreads = 32 * kInnerWarps;
 constexpr int kInnerK = 32 * kInnerWarps;   // values of k per stage
 constexpr uint32_t kXPitch = kInnerK + 32, kAPitch = 2 * kInnerK + 64;      // bytes: a warp's accesses fall into different banks
-constexpr int kInnerStages = 2;
+constexpr int kInnerStages = 4;             // two where four would not leave room for another block on the SM
 
 // Four int8 values (one word) to two words of 16-bit values: 0, 1 and 2, 3.
 template <class H> __device__ __forceinline__ void widen_4(uint32_t w, uint32_t &lo, uint32_t &hi);
@@ -316,25 +322,32 @@ template <> __device__ __forceinline__ uint32_t pack_pair<__half>(float lo, floa
 
 // The power of two by which a row's inner products are divided, so that the largest lies in [2^13, 2^14): far from both ends
 // of the 16-bit types.  1 for a row of (nearly) zeros or one that has a value which is not finite.
-__device__ __forceinline__ float row_power(float top)
+__device__ __forceinline__ float row_power(float top, float &inverse)
 {
     const uint32_t e = (__float_as_uint(top) >> 23) & 0xFFu;
-    return e <= 14u || e == 255u ? 1.0f : __uint_as_float((e - 13u) << 23);
+    const bool plain = e <= 14u || e == 255u;
+    inverse = plain ? 1.0f : __uint_as_float((267u - e) << 23);        // 2^(13 + 127 - e), down to 2^-113
+    return plain ? 1.0f : __uint_as_float((e - 13u) << 23);
 }
 
 // Shared memory: the stages (rows, then ranks), afterwards the warps' sums [warp][row][kPartPitch]; behind them the item's
 // sums [row][pitch].
 constexpr int kPartPitch = kRankPart + 1;
 static __host__ __device__ inline uint32_t inner_stage(int pitch) { return kItemRows * kXPitch + (uint32_t)(pitch < kRankPart ? pitch : kRankPart) * kAPitch; }
+static __host__ __device__ inline int inner_stages(int pitch)
+{
+    return inner_stage(pitch) * kInnerStages <= 100u * 1024u ? kInnerStages : 2;
+}
 static __host__ __device__ inline uint32_t inner_sums_at(int pitch)
 {
-    const uint32_t a = kInnerStages * inner_stage(pitch), b = kInnerWarps * kItemRows * kPartPitch * 4u;
+    const uint32_t a = (uint32_t)inner_stages(pitch) * inner_stage(pitch), b = kInnerWarps * kItemRows * kPartPitch * 4u;
     return a > b ? a : b;
 }
 static inline size_t inner_smem(int pitch) { return inner_sums_at(pitch) + (size_t)kItemRows * pitch * sizeof(float); }
 
-template <class H>
-__global__ void __launch_bounds__(32 * kInnerWarps, 2)
+// R: ranks of a pass, the pitch up to 64.
+template <class H, int R>
+__global__ void __launch_bounds__(kInnerThreads, 2)
 inner_tiles_kernel(const Params p)
 {
     extern __shared__ __align__(16) uint8_t smem[];
@@ -351,7 +364,7 @@ inner_tiles_kernel(const Params p)
 
     // rows without an adapter come last (adapters are below 2^20)
     constexpr int kNone = 1 << 20;
-    const int mine = first + tid < p.m ? adapter_of(p, (first + tid) / p.rows_per_sample) : -1;
+    const int mine = first + tid < p.m ? adapter_of(p, sample_of(p, first + tid)) : -1;
     const int key = (mine < 0 ? kNone : mine) << 8 | tid;
     key_s[tid] = key;
     if (blockIdx.y == 0 && first + tid < p.m) p.row_adapter[first + tid] = mine;
@@ -401,97 +414,120 @@ inner_tiles_kernel(const Params p)
     }
     __syncthreads();
 
-    const uint32_t base = ptx::smem_u32(smem), stage_bytes = inner_stage(p.pitch);
-    const int steps = (p.cin + kInnerK - 1) / kInnerK;
+    const uint32_t stage_bytes = inner_stage(p.pitch), base = ptx::smem_u32(smem);
+    const int steps = (p.cin + kInnerK - 1) / kInnerK, stages = inner_stages(p.pitch);
     for (int it = blockIdx.y; it < items; it += gridDim.y) {
         const int at = item_s[it] & 0xFFFF, count = item_s[it] >> 16;
         const int a = sorted_s[at] >> 8;
-        const H *am = static_cast<const H *>(p.a) + (size_t)a * p.rank * p.cin;
-        for (int j0 = 0; j0 < p.pitch; j0 += kRankPart) {
-            const int ranks = p.pitch - j0 < kRankPart ? p.pitch - j0 : kRankPart;      // a multiple of 16
-            // 16-byte pieces: a row has kInnerK / 16 of them, a rank kInnerK / 8; zeros past cin and rank
-            auto fetch = [&](int step) {
-                const uint32_t dst = base + (uint32_t)(step % kInnerStages) * stage_bytes;
-                const int k0 = step * kInnerK;
-                for (int i = tid; i < kItemRows * (kInnerK / 16); i += 32 * kInnerWarps) {
-                    const int row = i / (kInnerK / 16), piece = i % (kInnerK / 16), k = k0 + 16 * piece;
-                    const bool there = row < count && k < p.cin;
-                    const int8_t *src = p.x + (first + (sorted_s[at + (row < count ? row : 0)] & 255)) * p.cin + (there ? k : 0);
-                    ptx::cp_async_16_or_zero(dst + (uint32_t)row * kXPitch + 16u * piece, src, there);
+        for (int j0 = 0; j0 < p.pitch; j0 += R) {
+            // Copies: two pieces of 16 bytes of the rows and R / 8 of the ranks per thread and stage, zeros past cin.  Rows past the
+            // item's and ranks past the adapter's repeat the last one: they end in sums that are not used.
+            const int xk = 16 * (tid & 15), ak = 8 * (tid & 31);
+            const int8_t *xsrc[2];
+            const H *asrc[R / 8];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int row = (tid >> 4) + 16 * i;
+                xsrc[i] = p.x + (first + (sorted_s[at + (row < count ? row : count - 1)] & 255)) * p.cin + xk;
+            }
+#pragma unroll
+            for (int i = 0; i < R / 8; ++i) {
+                const int j = j0 + (tid >> 5) + 8 * i;
+                asrc[i] = static_cast<const H *>(p.a) + ((size_t)a * p.rank + (j < p.rank ? j : p.rank - 1)) * p.cin + ak;
+            }
+            const uint32_t xdst = base + (uint32_t)(tid >> 4) * kXPitch + (uint32_t)xk;
+            const uint32_t adst = base + kItemRows * kXPitch + (uint32_t)(tid >> 5) * kAPitch + 2u * ak;
+            int k_next = 0;
+            uint32_t to = 0;
+            auto fetch = [&] {
+                if (k_next + kInnerK <= p.cin) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) ptx::cp_async_16(xdst + to + 16u * i * kXPitch, xsrc[i] + k_next);
+#pragma unroll
+                    for (int i = 0; i < R / 8; ++i) ptx::cp_async_16(adst + to + 8u * i * kAPitch, asrc[i] + k_next);
+                } else if (k_next < p.cin) {
+                    const bool xin = k_next + xk < p.cin, ain = k_next + ak < p.cin;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) ptx::cp_async_16_or_zero(xdst + to + 16u * i * kXPitch, xin ? xsrc[i] + k_next : p.x, xin);
+#pragma unroll
+                    for (int i = 0; i < R / 8; ++i) ptx::cp_async_16_or_zero(adst + to + 8u * i * kAPitch, ain ? (const void *)(asrc[i] + k_next) : p.a, ain);
                 }
-                for (int i = tid; i < ranks * (kInnerK / 8); i += 32 * kInnerWarps) {
-                    const int row = i / (kInnerK / 8), piece = i % (kInnerK / 8), k = k0 + 8 * piece;
-                    const bool there = j0 + row < p.rank && k < p.cin;
-                    ptx::cp_async_16_or_zero(dst + kItemRows * kXPitch + (uint32_t)row * kAPitch + 16u * piece,
-                                             am + (there ? (size_t)(j0 + row) * p.cin + k : 0), there);
-                }
-                ptx::cp_async_commit();
+                k_next += kInnerK;
+                to = to + stage_bytes == stages * stage_bytes ? 0u : to + stage_bytes;
+                ptx::cp_async_commit();         // (an empty group where there is no stage: the waits count groups)
             };
-            float acc[2][8][4];                 // [16 rows][8 ranks][...]
+            float acc[2][R / 8][4];             // [16 rows][8 ranks][...]
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
+                for (int j = 0; j < R / 8; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
-            fetch(0);
+            fetch();
+            if (stages > 2) { fetch(); fetch(); }
+            uint32_t st = 0;
             for (int step = 0; step < steps; ++step) {
-                if (step + 1 < steps) { fetch(step + 1); ptx::cp_async_wait<1>(); }
+                if (stages > 2) ptx::cp_async_wait<2>();
                 else ptx::cp_async_wait<0>();
-                __syncthreads();
-                const uint8_t *sx = smem + (uint32_t)(step % kInnerStages) * stage_bytes + 32 * warp + 8 * t;
-                const uint8_t *sa = smem + (uint32_t)(step % kInnerStages) * stage_bytes + kItemRows * kXPitch + 64 * warp + 16 * t;
-                uint32_t f[2][2][4];            // [16 rows][first, second 16 of k]
+                __syncthreads();                // the stage is there, and the one before it has been read
+                fetch();
+                const uint8_t *sx = smem + st * stage_bytes + 32 * warp + 8 * t;
+                const uint8_t *sa = smem + st * stage_bytes + kItemRows * kXPitch + 64 * warp + 16 * t;
+                uint4 b[R / 8];
+#pragma unroll
+                for (int j = 0; j < R / 8; ++j) b[j] = *reinterpret_cast<const uint4 *>(sa + (uint32_t)(8 * j + g) * kAPitch);
+                uint2 xv[2][2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) xv[i][h] = *reinterpret_cast<const uint2 *>(sx + (uint32_t)(16 * i + 8 * h + g) * kXPitch);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const uint2 lo = *reinterpret_cast<const uint2 *>(sx + (uint32_t)(16 * i + g) * kXPitch);
-                    const uint2 hi = *reinterpret_cast<const uint2 *>(sx + (uint32_t)(16 * i + 8 + g) * kXPitch);
-                    widen_4<H>(lo.x, f[i][0][0], f[i][0][2]);
-                    widen_4<H>(hi.x, f[i][0][1], f[i][0][3]);
-                    widen_4<H>(lo.y, f[i][1][0], f[i][1][2]);
-                    widen_4<H>(hi.y, f[i][1][1], f[i][1][3]);
+                    uint32_t f[2][4];
+                    widen_4<H>(xv[i][0].x, f[0][0], f[0][2]);
+                    widen_4<H>(xv[i][1].x, f[0][1], f[0][3]);
+                    widen_4<H>(xv[i][0].y, f[1][0], f[1][2]);
+                    widen_4<H>(xv[i][1].y, f[1][1], f[1][3]);
+#pragma unroll
+                    for (int j = 0; j < R / 8; ++j) mma_16<H>(acc[i][j], f[0], b[j].x, b[j].y);
+#pragma unroll
+                    for (int j = 0; j < R / 8; ++j) mma_16<H>(acc[i][j], f[1], b[j].z, b[j].w);
                 }
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (8 * j < ranks) {
-                        const uint4 b = *reinterpret_cast<const uint4 *>(sa + (uint32_t)(8 * j + g) * kAPitch);
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            mma_16<H>(acc[i][j], f[i][0], b.x, b.y);
-                            mma_16<H>(acc[i][j], f[i][1], b.z, b.w);
-                        }
-                    }
-                __syncthreads();                // the stage may be filled again
+                if (++st == (uint32_t)stages) st = 0;
             }
+            ptx::cp_async_wait<0>();
+            __syncthreads();                    // the sums take the stages' place
             float *own = part + (size_t)warp * kItemRows * kPartPitch;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (8 * j < ranks) {
+                for (int j = 0; j < R / 8; ++j)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) own[(16 * i + g + 8 * (e >> 1)) * kPartPitch + 8 * j + 2 * t + (e & 1)] = acc[i][j][e];
-                    }
+                    for (int e = 0; e < 4; ++e) own[(16 * i + g + 8 * (e >> 1)) * kPartPitch + 8 * j + 2 * t + (e & 1)] = acc[i][j][e];
             __syncthreads();
-            for (int i = tid; i < count * ranks; i += 32 * kInnerWarps) {
-                const int k = i / ranks, j = i - k * ranks;
+            for (int i = tid; i < count * R; i += kInnerThreads) {
+                const int k = i / R, j = i % R;
                 float s = 0.0f;
 #pragma unroll
                 for (int w = 0; w < kInnerWarps; ++w) s += part[(w * kItemRows + k) * kPartPitch + j];
-                sums[k * p.pitch + j0 + j] = s;
+                if (j0 + j < p.pitch) sums[k * p.pitch + j0 + j] = j0 + j < p.rank ? s : 0.0f;
             }
             __syncthreads();
         }
-        // a warp per row: the power, and the 16-bit values
-        for (int k = warp; k < count; k += kInnerWarps) {
-            const float *v = sums + k * p.pitch;
-            float top = 0.0f;
-            for (int j = lane; j < p.pitch; j += 32) top = norm::max_nan(top, fabsf(v[j]));
-            const float power = row_power(norm::warp_max(top)), by = 1.0f / power;
+        // eight lanes a row: the power, and the 16-bit values
+        const int k = tid >> 3, q = tid & 7;
+        const float *v = sums + (k < count ? k : 0) * p.pitch;
+        float top = 0.0f;
+        for (int j = q; j < p.pitch; j += 8) top = norm::max_nan(top, fabsf(v[j]));
+#pragma unroll
+        for (int d = 4; d > 0; d >>= 1) top = norm::max_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+        if (k < count) {
+            float by;
+            const float power = row_power(top, by);
             const long long r = first + (sorted_s[at + k] & 255);
-            if (lane == 0) p.power[r] = power;
+            if (q == 0) p.power[r] = power;
             uint32_t *out = static_cast<uint32_t *>(p.t16) + (size_t)r * p.terms * (p.pitch / 2);
-            for (int j = lane; j < p.pitch / 2; j += 32) {
+            for (int j = q; j < p.pitch / 2; j += 8) {
                 float lo = v[2 * j] * by, hi = v[2 * j + 1] * by;
                 for (int m = 0; m < p.terms; ++m) {
                     out[m * (p.pitch / 2) + j] = pack_pair<H>(lo, hi);
@@ -513,7 +549,8 @@ inner_tiles_kernel(const Params p)
 // Behind the chunks of K come those of the adapters: for each adapter of the tile the rows' inner products (zero for rows of
 // other adapters), as sums of 16-bit values (two, or three for binary32 outputs) side by side along K, against B
 // repeated as often.
-constexpr int kFillGroups = 4, kGroupWarps = 2, kFillWarps = kFillGroups * kGroupWarps, kEpiWarps = 8;
+constexpr int kFillGroups = 4, kGroupWarps = 2, kFillWarps = kFillGroups * kGroupWarps;
+constexpr int kEpiGroups = 4, kEpiWarps = 4 * kEpiGroups;
 constexpr int kFill0 = 2, kEpi0 = kFill0 + kFillWarps;
 constexpr int kTileThreads = 32 * (kEpi0 + kEpiWarps);
 constexpr int kStages = 4;
@@ -566,7 +603,7 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
 
     if (warp == 0) {
         if (lane < kStages) {
-            ptx::mbar_init(bar_full + 8 * lane, 1 + 2 * kGroupWarps);
+            ptx::mbar_init(bar_full + 8 * lane, 1 + 2 * kFillWarps);
             ptx::mbar_init(bar_empty + 8 * lane, 1);
         } else if (lane == 31) {
             ptx::mbar_init(bar_tfull, 1);
@@ -682,8 +719,9 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
         __syncwarp();
     } else if (warp < kEpi0) {
         // ---- fillers: weights, then the adapters' operands ----------------------------------------------------
-        // The stages of all units are numbered through, a group takes every fourth.  A thread has four half rows of
-        // 64 bytes: rows row0, row0 + 32, ...
+        // The stages of all units are numbered through.  A group takes every fourth of those with weights (its arrival counts
+        // for the others'), a thread four half rows of 64 bytes: rows row0, row0 + 32, ...  Those of the adapters, of which
+        // there are few, all groups fill together, a group 32 rows.
         const int f = threadIdx.x - 32 * kFill0, grp = f / (32 * kGroupWarps), ft = f % (32 * kGroupWarps);
         const int row0 = ft >> 1, half = ft & 1;
         const uint32_t full = ptx::map_to_rank(bar_full, 0);
@@ -700,8 +738,7 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
         auto publish = [&](uint32_t n, uint32_t arrivals) {
             ptx::fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0)
-                for (uint32_t i = 0; i < arrivals; ++i) ptx::mbar_arrive_cluster(full + 8 * (n % kStages));
+            if (lane == 0) ptx::mbar_arrive_cluster_n(full + 8 * (n % kStages), arrivals);
         };
         for (long long u = pair; u < units && ok; u += pairs) {
             const int mt = (int)(u / q.n_ctiles), ct = (int)(u % q.n_ctiles);
@@ -725,99 +762,83 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                     }
                 }
             };
-            // the tile's adapters and the rows' own, looked up a whole pass over K before they are needed
+            // the tile's adapters and this thread's row's own, looked up a whole pass over K before they are needed
             const int *list = p.list + (size_t)mt * kListInts;
-            int chunks = 0, mine[4], held[2];
+            int chunks = 0, mine = -1, held[2];
             auto look = [&] {
                 chunks = __ldcg(list) * per_adapter;
                 held[0] = __ldcg(list + 1);         // (what lies past the number is not used)
                 held[1] = __ldcg(list + 2);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const long long r = (long long)mt * kTile + (int)rank * 128 + row0 + 32 * i;
-                    mine[i] = r < p.m ? __ldcg(p.row_adapter + r) : -1;
-                }
+                const long long r = (long long)mt * kTile + (int)rank * 128 + row0 + 32 * grp;
+                mine = r < p.m ? __ldcg(p.row_adapter + r) : -1;
             };
             if (p.a && waited) look();
             int c = (int)(((uint32_t)grp - seq) % kFillGroups);
             if (c < q.kc) fetch(c);
             for (; c < q.kc; c += kFillGroups) {
                 const uint32_t n = seq + (uint32_t)c;
-                // expanded while the stage is still in use: only the stores are behind the wait
-                uint4 wide[4][4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        invalid |= (code[i][j] >> 1) & ~code[i][j] & 0x55555555u;
-                        wide[i][j] = expand_16(code[i][j]);
-                    }
-                if (c + kFillGroups < q.kc) fetch(c + kFillGroups);
                 if (!enter(n)) { ok = false; break; }
                 uint8_t *dst = smem + (n % kStages) * kStage + kHalfStage;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (row0 + 32 * i < rows) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            *reinterpret_cast<uint4 *>(dst + tc::swz_offset((uint32_t)(row0 + 32 * i), (uint32_t)(half * 4 + j), 128u)) = wide[i][j];
+                        for (int j = 0; j < 4; ++j) {
+                            invalid |= (code[i][j] >> 1) & ~code[i][j] & 0x55555555u;
+                            *reinterpret_cast<uint4 *>(dst + tc::swz_offset((uint32_t)(row0 + 32 * i), (uint32_t)(half * 4 + j), 128u)) = expand_16(code[i][j]);
+                        }
                     }
-                publish(n, 1);
+                if (c + kFillGroups < q.kc) fetch(c + kFillGroups);
+                publish(n, kFillGroups);
             }
             seq += (uint32_t)q.kc;
             if (!ok || !p.a) continue;
             if (!waited) { ptx::grid_dep_wait(); waited = true; look(); }
-            for (c = (int)(((uint32_t)grp - seq) % kFillGroups); c < chunks; c += kFillGroups) {
-                const uint32_t n = seq + (uint32_t)c;
-                const int i_ad = c / per_adapter, part = c - i_ad * per_adapter;
+            const int row = row0 + 32 * grp;
+            const long long r = (long long)mt * kTile + (int)rank * 128 + row;
+            const bool there = row < rows && o0 + row < p.cout, wide_b = (p.rank & 7) == 0;
+            for (int i_ad = 0, part = 0, c2 = 0; c2 < chunks; ++c2) {
+                const uint32_t n = seq + (uint32_t)c2;
                 const int a = i_ad == 0 ? held[0] : (i_ad == 1 ? held[1] : __ldcg(list + 1 + i_ad));
                 const int e0 = part * 64 + half * 32;
                 if (!enter(n)) { ok = false; break; }
                 const uint32_t dst = base + (n % kStages) * kStage;
-                const bool wide_b = (p.rank & 7) == 0;
+                const H *t16 = static_cast<const H *>(p.t16) + (size_t)(mine == a ? r : 0) * k2;
+                const H *b = static_cast<const H *>(p.b) + ((size_t)a * p.cout + (there ? o0 + row : 0)) * p.rank;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int row = row0 + 32 * i;
-                    const long long r = (long long)mt * kTile + (int)rank * 128 + row;
-                    const bool there = row < rows && o0 + row < p.cout;
-                    const H *t16 = static_cast<const H *>(p.t16) + (size_t)(mine[i] == a ? r : 0) * k2;
-                    const H *b = static_cast<const H *>(p.b) + ((size_t)a * p.cout + (there ? o0 + row : 0)) * p.rank;
+                for (int k = 0; k < 4; ++k) {
+                    const int e = e0 + 8 * k, j = e - (e >= p.pitch ? p.pitch : 0) - (e >= 2 * p.pitch ? p.pitch : 0);
+                    const uint32_t off = tc::swz_offset((uint32_t)row, (uint32_t)(half * 4 + k), 128u);
+                    const bool t_in = e < k2 && mine == a, b_in = e < k2 && there && j < p.rank;
+                    ptx::cp_async_16_or_zero(dst + off, t16 + (t_in ? e : 0), t_in);
+                    if (wide_b) {
+                        ptx::cp_async_16_or_zero(dst + kHalfStage + off, b + (b_in ? j : 0), b_in);
+                    } else {
+                        uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int e = e0 + 8 * k, j = e - (e >= p.pitch ? p.pitch : 0) - (e >= 2 * p.pitch ? p.pitch : 0);
-                        const uint32_t off = tc::swz_offset((uint32_t)row, (uint32_t)(half * 4 + k), 128u);
-                        const bool t_in = e < k2 && mine[i] == a, b_in = e < k2 && there && j < p.rank;
-                        ptx::cp_async_16_or_zero(dst + off, t16 + (t_in ? e : 0), t_in);
-                        if (wide_b) {
-                            ptx::cp_async_16_or_zero(dst + kHalfStage + off, b + (b_in ? j : 0), b_in);
-                        } else {
-                            uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-                            for (int s = 0; s < 8; ++s)
-                                if (b_in && j + s < p.rank) w[s >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short *>(b) + j + s) << (16 * (s & 1));
-                            ptx::sts_128(dst + kHalfStage + off, w[0], w[1], w[2], w[3]);
-                        }
+                        for (int s = 0; s < 8; ++s)
+                            if (b_in && j + s < p.rank) w[s >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short *>(b) + j + s) << (16 * (s & 1));
+                        ptx::sts_128(dst + kHalfStage + off, w[0], w[1], w[2], w[3]);
                     }
                 }
                 ptx::cp_async_wait_all();
                 // what is not finite in B counts as zero
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int k = 0; k < 4; ++k) {
+                    const uint32_t at = dst + kHalfStage + tc::swz_offset((uint32_t)row, (uint32_t)(half * 4 + k), 128u);
+                    const int4 v = ptx::lds_128(at);
+                    uint32_t w[4] = {(uint32_t)v.x, (uint32_t)v.y, (uint32_t)v.z, (uint32_t)v.w};
+                    constexpr uint32_t top = std::is_same<H, __nv_bfloat16>::value ? 0x7F80u : 0x7C00u;    // its exponent
+                    bool hit = false;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t at = dst + kHalfStage + tc::swz_offset((uint32_t)(row0 + 32 * i), (uint32_t)(half * 4 + k), 128u);
-                        const int4 v = ptx::lds_128(at);
-                        uint32_t w[4] = {(uint32_t)v.x, (uint32_t)v.y, (uint32_t)v.z, (uint32_t)v.w};
-                        constexpr uint32_t top = std::is_same<H, __nv_bfloat16>::value ? 0x7F80u : 0x7C00u;    // its exponent
-                        bool hit = false;
-#pragma unroll
-                        for (int s = 0; s < 4; ++s) {
-                            if ((w[s] & top) == top) { w[s] &= 0xFFFF0000u; hit = true; }
-                            if (((w[s] >> 16) & top) == top) { w[s] &= 0x0000FFFFu; hit = true; }
-                        }
-                        if (hit) { bad = true; ptx::sts_128(at, w[0], w[1], w[2], w[3]); }
+                    for (int s = 0; s < 4; ++s) {
+                        if ((w[s] & top) == top) { w[s] &= 0xFFFF0000u; hit = true; }
+                        if (((w[s] >> 16) & top) == top) { w[s] &= 0x0000FFFFu; hit = true; }
                     }
-                publish(n, ft < 32 && rank == 0 ? 2u : 1u);     // (the loader's arrival among them)
+                    if (hit) { bad = true; ptx::sts_128(at, w[0], w[1], w[2], w[3]); }
+                }
+                publish(n, f < 32 && rank == 0 ? 2u : 1u);      // (the loader's arrival among them)
+                if (++part == per_adapter) { part = 0; ++i_ad; }
             }
             seq += (uint32_t)chunks;
         }
@@ -825,13 +846,14 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
         __syncwarp();
     } else {
         // ---- epilogue --------------------------------------------------------------------------------------------
-        // Two groups of four warps, a warp per quarter of the rows: pieces of 32 outputs, every second one a group's.
+        // Four groups of four warps, a warp per quarter of the rows: pieces of 32 outputs, every fourth one a group's.
         const int e = warp - kEpi0, quarter = warp & 3, grp = e >> 2;
         uint8_t *slab = smem + kOffSlab + (size_t)e * kSlab;
         const uint32_t slab_addr = ptx::smem_u32(slab);
         const uint32_t t_lane = tmem + ((uint32_t)(quarter * 32) << 16);
         const uint32_t tempty = ptx::map_to_rank(bar_tempty, 0);
         constexpr uint32_t kRowBytes = 32u * (uint32_t)sizeof(Y);
+        const bool alpha_wide = (reinterpret_cast<uintptr_t>(p.alpha) & 15u) == 0;
         if (p.chained) ptx::grid_dep_wait();
         uint32_t done = 0;
         for (long long u = pair; u < units; u += pairs, ++done) {
@@ -841,7 +863,7 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
             float fac = 0.0f, ad = 0.0f;
             bool with = false;
             if (r < p.m) {
-                const long long s = r / p.rows_per_sample;
+                const int s = sample_of(p, r);
                 fac = row_factor(p, s);
                 if (adapters) {
                     const int a = __ldcg(p.row_adapter + r);
@@ -858,43 +880,46 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
             };
             if (grp >= pieces) release();
 #pragma unroll 1
-            for (int pc = grp; pc < pieces; pc += 2) {
+            for (int pc = grp; pc < pieces; pc += kEpiGroups) {
                 const int at = ct * q.nt + pc * 32;
-                uint32_t v[32], w[32];
-                ptx::tmem_ld_x32(t_lane + (uint32_t)pc * 32u, v);
-                if (adapters) ptx::tmem_ld_x32(t_lane + kD2 + (uint32_t)pc * 32u, w);
-                ptx::tmem_wait_ld();
-                if (pc + 2 >= pieces) release();
-                float y[32];
-#pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    float4 al = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    if (at + i < p.cout) {          // (whole groups of eight outputs)
-                        al.x = __ldg(p.alpha + at + i); al.y = __ldg(p.alpha + at + i + 1);
-                        al.z = __ldg(p.alpha + at + i + 2); al.w = __ldg(p.alpha + at + i + 3);
-                    }
-                    y[i] = (float)(int)v[i] * al.x * fac;
-                    y[i + 1] = (float)(int)v[i + 1] * al.y * fac;
-                    y[i + 2] = (float)(int)v[i + 2] * al.z * fac;
-                    y[i + 3] = (float)(int)v[i + 3] * al.w * fac;
-                }
-                if (with) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) y[i] += ad * __uint_as_float(w[i]);
-                }
                 ptx::bulk_wait_read0();             // the previous store has read the slab
                 __syncwarp();
-                if constexpr (sizeof(Y) == 4) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        *reinterpret_cast<float4 *>(slab + tc::swz_offset((uint32_t)lane, (uint32_t)j, 128u)) =
-                            make_float4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
-                } else {
+                for (int h = 0; h < 32; h += 16) {
+                    uint32_t v[16], w[16];
+                    ptx::tmem_ld_x16(t_lane + (uint32_t)(pc * 32 + h), v);
+                    if (adapters) ptx::tmem_ld_x16(t_lane + kD2 + (uint32_t)(pc * 32 + h), w);
+                    float al[16];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        *reinterpret_cast<uint4 *>(slab + tc::swz_offset((uint32_t)lane, (uint32_t)j, 64u)) =
-                            make_uint4(pack_pair<Y>(y[8 * j], y[8 * j + 1]), pack_pair<Y>(y[8 * j + 2], y[8 * j + 3]),
-                                       pack_pair<Y>(y[8 * j + 4], y[8 * j + 5]), pack_pair<Y>(y[8 * j + 6], y[8 * j + 7]));
+                    for (int i = 0; i < 16; i += 4) {
+                        float4 a4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        if (at + h + i < p.cout) {          // (whole groups of eight outputs)
+                            const float *src = p.alpha + at + h + i;
+                            if (alpha_wide) a4 = __ldg(reinterpret_cast<const float4 *>(src));
+                            else a4 = make_float4(__ldg(src), __ldg(src + 1), __ldg(src + 2), __ldg(src + 3));
+                        }
+                        al[i] = a4.x; al[i + 1] = a4.y; al[i + 2] = a4.z; al[i + 3] = a4.w;
+                    }
+                    ptx::tmem_wait_ld();
+                    if (h && pc + kEpiGroups >= pieces) release();
+                    float y[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        y[i] = (float)(int)v[i] * al[i] * fac;
+                        if (with) y[i] += ad * __uint_as_float(w[i]);
+                    }
+                    if constexpr (sizeof(Y) == 4) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            *reinterpret_cast<float4 *>(slab + tc::swz_offset((uint32_t)lane, (uint32_t)(h / 4 + j), 128u)) =
+                                make_float4(y[4 * j], y[4 * j + 1], y[4 * j + 2], y[4 * j + 3]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            *reinterpret_cast<uint4 *>(slab + tc::swz_offset((uint32_t)lane, (uint32_t)(h / 8 + j), 64u)) =
+                                make_uint4(pack_pair<Y>(y[8 * j], y[8 * j + 1]), pack_pair<Y>(y[8 * j + 2], y[8 * j + 3]),
+                                           pack_pair<Y>(y[8 * j + 4], y[8 * j + 5]), pack_pair<Y>(y[8 * j + 6], y[8 * j + 7]));
+                    }
                 }
                 if (q.store) {
                     ptx::fence_proxy_async_smem();

@@ -2423,6 +2423,18 @@ static size_t workspace_bytes(long long m, int rank)
     return t16_bytes(m, rank) + 2 * round256((size_t)m * sizeof(float)) + round256((size_t)row_tiles(m) * kListInts * sizeof(int));
 }
 
+template <class H, int R>
+static cudaError_t launch_inner(const Params &p, dim3 grid, cudaStream_t st)
+{
+    const cudaError_t e = raise_smem_limit(inner_tiles_kernel<H, R>, (int)inner_smem(kMaxRank));
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[1];
+    fill_launch_cfg(cfg, attr, 1, kInnerThreads, inner_smem(p.pitch), st, true);
+    cfg.gridDim = grid;
+    return cudaLaunchKernelEx(&cfg, inner_tiles_kernel<H, R>, p);
+}
+
 template <class H, class Y>
 static prom_status run_tiles(Params &p, int y_type, const DeviceInfo &d, cudaStream_t st)
 {
@@ -2475,13 +2487,14 @@ static prom_status run_tiles(Params &p, int y_type, const DeviceInfo &d, cudaStr
         p.power = reinterpret_cast<float *>(ws + t16_bytes(p.m, p.rank));
         p.row_adapter = reinterpret_cast<int *>(ws + t16_bytes(p.m, p.rank) + round256((size_t)p.m * sizeof(float)));
         p.list = reinterpret_cast<int *>(ws + t16_bytes(p.m, p.rank) + 2 * round256((size_t)p.m * sizeof(float)));
-        if (raise_smem_limit(inner_tiles_kernel<H>, (int)inner_smem(kMaxRank)) != cudaSuccess) return PROM_ERR_CUDA;
-        fill_launch_cfg(cfg, attr, 1, 32 * kInnerWarps, inner_smem(p.pitch), st, true);
         // a tile's items over several blocks: eight of a run of 256 rows, more where there are few tiles
         long long share = (2ll * d.sms + q.n_mtiles - 1) / q.n_mtiles;
         share = share < 8 ? 8 : (share > 32 ? 32 : share);
-        cfg.gridDim = dim3((unsigned)q.n_mtiles, (unsigned)share);
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, inner_tiles_kernel<H>, p);
+        const dim3 grid((unsigned)q.n_mtiles, (unsigned)share);
+        const cudaError_t e = p.pitch <= 16   ? launch_inner<H, 16>(p, grid, st)
+                              : p.pitch <= 32 ? launch_inner<H, 32>(p, grid, st)
+                              : p.pitch <= 48 ? launch_inner<H, 48>(p, grid, st)
+                                              : launch_inner<H, 64>(p, grid, st);
         ++g_launches;
         if (e != cudaSuccess) return cuda_status(e);
         p.chained = 1;

@@ -258,20 +258,22 @@ proj_rows_kernel(const Params p)
 // ---- many rows: inner products ----------------------------------------------------------------------------------
 // Rows in tiles of 256.  A block sorts the tile's rows by their adapter (a row's place is the number of smaller keys), so
 // that any order of requests costs what runs of requests cost: an item is up to 32 rows of one adapter, and the items go
-// round the blocks of a tile.  K comes in stages of 256 by asynchronous copies of 16 bytes (a bulk copy per row and rank took
-// twice as long: they are a few hundred bytes each); each of the eight warps multiplies its 32 of them with the warp-level
-// 16-bit MMA, rows as A (int8 values are exact in both 16-bit types) and the adapter as B, and the warps' sums are added at
-// the end.  A thread's 8 bytes of a row and 16 of the adapter are 8 neighbouring values of k, whose order inside the MMAs
-// is free.  The sums are then split into 16-bit values once, for all the projection's tiles of outputs.
+// round the blocks of a tile.  K comes in stages of 256 (128 from 48 ranks on) by asynchronous copies of 16 bytes (a bulk copy
+// per row and rank took twice as long: they are a few hundred bytes each); each of the eight warps multiplies an eighth of
+// them with the warp-level 16-bit MMA, rows as A (int8 values are exact in both 16-bit types) and the adapter as B, and the
+// warps' sums are added at the end.  A thread's 4 KS bytes of a row and 8 KS of the adapter are neighbouring values of k,
+// whose order inside the MMAs is free.  The sums are then split into 16-bit values once, for all the projection's tiles of outputs.
 constexpr int kTile = 256;
 constexpr int kItemRows = 32;
 constexpr int kListInts = kTile + 1;
 constexpr int kInnerWarps = 8;
 constexpr int kRankPart = 64;               // ranks of one pass over K
 constexpr int kInnerThreads = 32 * kInnerWarps;
-constexpr int kInnerK = 32 * kInnerWarps;   // values of k per stage
-constexpr uint32_t kXPitch = kInnerK + 32, kAPitch = 2 * kInnerK + 64;      // bytes: a warp's accesses fall into different banks
-constexpr int kInnerStages = 4;             // two where four would not leave room for another block on the SM
+constexpr int kInnerStages = 4;
+// KS: MMA steps (16 values of k) per warp and stage.
+static __host__ __device__ constexpr int inner_ks(int r) { return r >= 48 ? 1 : 2; }
+static __host__ __device__ constexpr uint32_t x_pitch(int ks) { return 144u * ks; }     // bytes: a warp's accesses fall into
+static __host__ __device__ constexpr uint32_t a_pitch(int ks) { return 288u * ks; }     // different banks
 
 // Four int8 values (one word) to two words of 16-bit values: 0, 1 and 2, 3.
 template <class H> __device__ __forceinline__ void widen_4(uint32_t w, uint32_t &lo, uint32_t &hi);
@@ -333,17 +335,13 @@ __device__ __forceinline__ float row_power(float top, float &inverse)
 // Shared memory: the stages (rows, then ranks), afterwards the warps' sums [warp][row][kPartPitch]; behind them the item's
 // sums [row][pitch].
 constexpr int kPartPitch = kRankPart + 1;
-static __host__ __device__ inline uint32_t inner_stage(int pitch) { return kItemRows * kXPitch + (uint32_t)(pitch < kRankPart ? pitch : kRankPart) * kAPitch; }
-static __host__ __device__ inline int inner_stages(int pitch)
+static __host__ __device__ constexpr uint32_t inner_stage(int r) { return kItemRows * x_pitch(inner_ks(r)) + (uint32_t)r * a_pitch(inner_ks(r)); }
+static __host__ __device__ constexpr uint32_t inner_sums_at(int r)
 {
-    return inner_stage(pitch) * kInnerStages <= 100u * 1024u ? kInnerStages : 2;
+    return kInnerStages * inner_stage(r) > kInnerWarps * kItemRows * kPartPitch * 4u ? kInnerStages * inner_stage(r)
+                                                                                    : kInnerWarps * kItemRows * kPartPitch * 4u;
 }
-static __host__ __device__ inline uint32_t inner_sums_at(int pitch)
-{
-    const uint32_t a = (uint32_t)inner_stages(pitch) * inner_stage(pitch), b = kInnerWarps * kItemRows * kPartPitch * 4u;
-    return a > b ? a : b;
-}
-static inline size_t inner_smem(int pitch) { return inner_sums_at(pitch) + (size_t)kItemRows * pitch * sizeof(float); }
+static constexpr size_t inner_smem(int r, int pitch) { return inner_sums_at(r) + (size_t)kItemRows * pitch * sizeof(float); }
 
 // R: ranks of a pass, the pitch up to 64.
 template <class H, int R>
@@ -351,7 +349,7 @@ __global__ void __launch_bounds__(kInnerThreads, 2)
 inner_tiles_kernel(const Params p)
 {
     extern __shared__ __align__(16) uint8_t smem[];
-    float *part = reinterpret_cast<float *>(smem), *sums = reinterpret_cast<float *>(smem + inner_sums_at(p.pitch));
+    float *part = reinterpret_cast<float *>(smem), *sums = reinterpret_cast<float *>(smem + inner_sums_at(R));
     __shared__ __align__(16) int key_s[kTile];
     __shared__ int sorted_s[kTile + 1];         // adapter << 8 | row
     __shared__ unsigned start_s[kTile / 32];    // places where another adapter begins
@@ -414,46 +412,50 @@ inner_tiles_kernel(const Params p)
     }
     __syncthreads();
 
-    const uint32_t stage_bytes = inner_stage(p.pitch), base = ptx::smem_u32(smem);
-    const int steps = (p.cin + kInnerK - 1) / kInnerK, stages = inner_stages(p.pitch);
+    constexpr int KS = inner_ks(R), kInnerK = 16 * KS * kInnerWarps, kXRows = 32 / KS, kARows = 16 / KS, kACopies = R / kARows;
+    constexpr uint32_t kXPitch = x_pitch(KS), kAPitch = a_pitch(KS), stage_bytes = inner_stage(R);
+    const uint32_t base = ptx::smem_u32(smem);
+    const int steps = (p.cin + kInnerK - 1) / kInnerK;
     for (int it = blockIdx.y; it < items; it += gridDim.y) {
         const int at = item_s[it] & 0xFFFF, count = item_s[it] >> 16;
         const int a = sorted_s[at] >> 8;
         for (int j0 = 0; j0 < p.pitch; j0 += R) {
-            // Copies: two pieces of 16 bytes of the rows and R / 8 of the ranks per thread and stage, zeros past cin.  Rows past the
-            // item's and ranks past the adapter's repeat the last one: they end in sums that are not used.
-            const int xk = 16 * (tid & 15), ak = 8 * (tid & 31);
-            const int8_t *xsrc[2];
-            const H *asrc[R / 8];
+            // Copies: KS pieces of 16 bytes of the rows and R KS / 16 of the ranks per thread and stage, zeros past cin.  Rows past
+            // the item's and ranks past the adapter's repeat the last one: they end in sums that are not used.
+            const int xk = 16 * (tid % (8 * KS)), ak = 8 * (tid % (16 * KS)), xrow = tid / (8 * KS), arow = tid / (16 * KS);
+            const int8_t *xsrc[KS];
+            const H *asrc[kACopies];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int row = (tid >> 4) + 16 * i;
+            for (int i = 0; i < KS; ++i) {
+                const int row = xrow + kXRows * i;
                 xsrc[i] = p.x + (first + (sorted_s[at + (row < count ? row : count - 1)] & 255)) * p.cin + xk;
             }
 #pragma unroll
-            for (int i = 0; i < R / 8; ++i) {
-                const int j = j0 + (tid >> 5) + 8 * i;
+            for (int i = 0; i < kACopies; ++i) {
+                const int j = j0 + arow + kARows * i;
                 asrc[i] = static_cast<const H *>(p.a) + ((size_t)a * p.rank + (j < p.rank ? j : p.rank - 1)) * p.cin + ak;
             }
-            const uint32_t xdst = base + (uint32_t)(tid >> 4) * kXPitch + (uint32_t)xk;
-            const uint32_t adst = base + kItemRows * kXPitch + (uint32_t)(tid >> 5) * kAPitch + 2u * ak;
+            const uint32_t xdst = base + (uint32_t)xrow * kXPitch + (uint32_t)xk;
+            const uint32_t adst = base + kItemRows * kXPitch + (uint32_t)arow * kAPitch + 2u * ak;
             int k_next = 0;
             uint32_t to = 0;
             auto fetch = [&] {
                 if (k_next + kInnerK <= p.cin) {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) ptx::cp_async_16(xdst + to + 16u * i * kXPitch, xsrc[i] + k_next);
+                    for (int i = 0; i < KS; ++i) ptx::cp_async_16(xdst + to + (uint32_t)(kXRows * i) * kXPitch, xsrc[i] + k_next);
 #pragma unroll
-                    for (int i = 0; i < R / 8; ++i) ptx::cp_async_16(adst + to + 8u * i * kAPitch, asrc[i] + k_next);
+                    for (int i = 0; i < kACopies; ++i) ptx::cp_async_16(adst + to + (uint32_t)(kARows * i) * kAPitch, asrc[i] + k_next);
                 } else if (k_next < p.cin) {
                     const bool xin = k_next + xk < p.cin, ain = k_next + ak < p.cin;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) ptx::cp_async_16_or_zero(xdst + to + 16u * i * kXPitch, xin ? xsrc[i] + k_next : p.x, xin);
+                    for (int i = 0; i < KS; ++i)
+                        ptx::cp_async_16_or_zero(xdst + to + (uint32_t)(kXRows * i) * kXPitch, xin ? xsrc[i] + k_next : p.x, xin);
 #pragma unroll
-                    for (int i = 0; i < R / 8; ++i) ptx::cp_async_16_or_zero(adst + to + 8u * i * kAPitch, ain ? (const void *)(asrc[i] + k_next) : p.a, ain);
+                    for (int i = 0; i < kACopies; ++i)
+                        ptx::cp_async_16_or_zero(adst + to + (uint32_t)(kARows * i) * kAPitch, ain ? (const void *)(asrc[i] + k_next) : p.a, ain);
                 }
                 k_next += kInnerK;
-                to = to + stage_bytes == stages * stage_bytes ? 0u : to + stage_bytes;
+                to = to + stage_bytes == kInnerStages * stage_bytes ? 0u : to + stage_bytes;
                 ptx::cp_async_commit();         // (an empty group where there is no stage: the waits count groups)
             };
             float acc[2][R / 8][4];             // [16 rows][8 ranks][...]
@@ -463,37 +465,50 @@ inner_tiles_kernel(const Params p)
                 for (int j = 0; j < R / 8; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[i][j][e] = 0.0f;
-            fetch();
-            if (stages > 2) { fetch(); fetch(); }
+#pragma unroll
+            for (int i = 0; i < kInnerStages - 1; ++i) fetch();
             uint32_t st = 0;
             for (int step = 0; step < steps; ++step) {
-                if (stages > 2) ptx::cp_async_wait<2>();
-                else ptx::cp_async_wait<0>();
+                ptx::cp_async_wait<kInnerStages - 2>();
                 __syncthreads();                // the stage is there, and the one before it has been read
                 fetch();
-                const uint8_t *sx = smem + st * stage_bytes + 32 * warp + 8 * t;
-                const uint8_t *sa = smem + st * stage_bytes + kItemRows * kXPitch + 64 * warp + 16 * t;
-                uint4 b[R / 8];
+                const uint8_t *sx = smem + st * stage_bytes + KS * (16 * warp + 4 * t);
+                const uint8_t *sa = smem + st * stage_bytes + kItemRows * kXPitch + KS * (32 * warp + 8 * t);
+                uint2 b[R / 8][KS];
 #pragma unroll
-                for (int j = 0; j < R / 8; ++j) b[j] = *reinterpret_cast<const uint4 *>(sa + (uint32_t)(8 * j + g) * kAPitch);
-                uint2 xv[2][2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) xv[i][h] = *reinterpret_cast<const uint2 *>(sx + (uint32_t)(16 * i + 8 * h + g) * kXPitch);
+                for (int j = 0; j < R / 8; ++j) {
+                    if constexpr (KS == 2) {
+                        const uint4 v = *reinterpret_cast<const uint4 *>(sa + (uint32_t)(8 * j + g) * kAPitch);
+                        b[j][0] = make_uint2(v.x, v.y);
+                        b[j][1] = make_uint2(v.z, v.w);
+                    } else {
+                        b[j][0] = *reinterpret_cast<const uint2 *>(sa + (uint32_t)(8 * j + g) * kAPitch);
+                    }
+                }
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    uint32_t f[2][4];
-                    widen_4<H>(xv[i][0].x, f[0][0], f[0][2]);
-                    widen_4<H>(xv[i][1].x, f[0][1], f[0][3]);
-                    widen_4<H>(xv[i][0].y, f[1][0], f[1][2]);
-                    widen_4<H>(xv[i][1].y, f[1][1], f[1][3]);
+                    uint32_t xv[2][KS];
 #pragma unroll
-                    for (int j = 0; j < R / 8; ++j) mma_16<H>(acc[i][j], f[0], b[j].x, b[j].y);
+                    for (int h = 0; h < 2; ++h) {
+                        const uint8_t *src = sx + (uint32_t)(16 * i + 8 * h + g) * kXPitch;
+                        if constexpr (KS == 2) {
+                            const uint2 v = *reinterpret_cast<const uint2 *>(src);
+                            xv[h][0] = v.x;
+                            xv[h][1] = v.y;
+                        } else {
+                            xv[h][0] = *reinterpret_cast<const uint32_t *>(src);
+                        }
+                    }
 #pragma unroll
-                    for (int j = 0; j < R / 8; ++j) mma_16<H>(acc[i][j], f[1], b[j].z, b[j].w);
+                    for (int s = 0; s < KS; ++s) {
+                        uint32_t f[4];
+                        widen_4<H>(xv[0][s], f[0], f[2]);
+                        widen_4<H>(xv[1][s], f[1], f[3]);
+#pragma unroll
+                        for (int j = 0; j < R / 8; ++j) mma_16<H>(acc[i][j], f, b[j][s].x, b[j][s].y);
+                    }
                 }
-                if (++st == (uint32_t)stages) st = 0;
+                st = (st + 1) % kInnerStages;
             }
             ptx::cp_async_wait<0>();
             __syncthreads();                    // the sums take the stages' place
@@ -797,35 +812,12 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
             const int row = row0 + 32 * grp;
             const long long r = (long long)mt * kTile + (int)rank * 128 + row;
             const bool there = row < rows && o0 + row < p.cout, wide_b = (p.rank & 7) == 0;
-            for (int i_ad = 0, part = 0, c2 = 0; c2 < chunks; ++c2) {
-                const uint32_t n = seq + (uint32_t)c2;
-                const int a = i_ad == 0 ? held[0] : (i_ad == 1 ? held[1] : __ldcg(list + 1 + i_ad));
-                const int e0 = part * 64 + half * 32;
-                if (!enter(n)) { ok = false; break; }
-                const uint32_t dst = base + (n % kStages) * kStage;
-                const H *t16 = static_cast<const H *>(p.t16) + (size_t)(mine == a ? r : 0) * k2;
-                const H *b = static_cast<const H *>(p.b) + ((size_t)a * p.cout + (there ? o0 + row : 0)) * p.rank;
+            const uint32_t off0 = tc::swz_offset((uint32_t)row, (uint32_t)(half * 4), 128u);       // piece k: off0 ^ 16 k
+            // a chunk is announced while the next two's copies are on their way
+            auto land = [&](uint32_t n) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int e = e0 + 8 * k, j = e - (e >= p.pitch ? p.pitch : 0) - (e >= 2 * p.pitch ? p.pitch : 0);
-                    const uint32_t off = tc::swz_offset((uint32_t)row, (uint32_t)(half * 4 + k), 128u);
-                    const bool t_in = e < k2 && mine == a, b_in = e < k2 && there && j < p.rank;
-                    ptx::cp_async_16_or_zero(dst + off, t16 + (t_in ? e : 0), t_in);
-                    if (wide_b) {
-                        ptx::cp_async_16_or_zero(dst + kHalfStage + off, b + (b_in ? j : 0), b_in);
-                    } else {
-                        uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-                        for (int s = 0; s < 8; ++s)
-                            if (b_in && j + s < p.rank) w[s >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short *>(b) + j + s) << (16 * (s & 1));
-                        ptx::sts_128(dst + kHalfStage + off, w[0], w[1], w[2], w[3]);
-                    }
-                }
-                ptx::cp_async_wait_all();
-                // what is not finite in B counts as zero
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t at = dst + kHalfStage + tc::swz_offset((uint32_t)row, (uint32_t)(half * 4 + k), 128u);
+                for (int k = 0; k < 4; ++k) {       // what is not finite in B counts as zero
+                    const uint32_t at = base + (n % kStages) * kStage + kHalfStage + (off0 ^ (16u * k));
                     const int4 v = ptx::lds_128(at);
                     uint32_t w[4] = {(uint32_t)v.x, (uint32_t)v.y, (uint32_t)v.z, (uint32_t)v.w};
                     constexpr uint32_t top = std::is_same<H, __nv_bfloat16>::value ? 0x7F80u : 0x7C00u;    // its exponent
@@ -838,8 +830,41 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                     if (hit) { bad = true; ptx::sts_128(at, w[0], w[1], w[2], w[3]); }
                 }
                 publish(n, f < 32 && rank == 0 ? 2u : 1u);      // (the loader's arrival among them)
+            };
+            for (int i_ad = 0, part = 0, c2 = 0; c2 < chunks; ++c2) {
+                const uint32_t n = seq + (uint32_t)c2;
+                const int a = i_ad == 0 ? held[0] : (i_ad == 1 ? held[1] : __ldcg(list + 1 + i_ad));
+                const int e0 = part * 64 + half * 32;
+                if (!enter(n)) { ok = false; break; }
+                const uint32_t dst = base + (n % kStages) * kStage;
+                const H *t16 = static_cast<const H *>(p.t16) + (size_t)(mine == a ? r : 0) * k2;
+                const H *b = static_cast<const H *>(p.b) + ((size_t)a * p.cout + (there ? o0 + row : 0)) * p.rank;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int e = e0 + 8 * k, j = e - (e >= p.pitch ? p.pitch : 0) - (e >= 2 * p.pitch ? p.pitch : 0);
+                    const uint32_t off = off0 ^ (16u * k);
+                    const bool t_in = e < k2 && mine == a, b_in = e < k2 && there && j < p.rank;
+                    ptx::cp_async_16_or_zero(dst + off, t16 + (t_in ? e : 0), t_in);
+                    if (wide_b) {
+                        ptx::cp_async_16_or_zero(dst + kHalfStage + off, b + (b_in ? j : 0), b_in);
+                    } else {
+                        uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+                        for (int s = 0; s < 8; ++s)
+                            if (b_in && j + s < p.rank) w[s >> 1] |= (uint32_t)__ldg(reinterpret_cast<const unsigned short *>(b) + j + s) << (16 * (s & 1));
+                        ptx::sts_128(dst + kHalfStage + off, w[0], w[1], w[2], w[3]);
+                    }
+                }
+                ptx::cp_async_commit();
+                if (c2 > 1) {
+                    ptx::cp_async_wait<2>();
+                    land(n - 2);
+                }
                 if (++part == per_adapter) { part = 0; ++i_ad; }
             }
+            ptx::cp_async_wait_all();
+            if (ok && chunks > 1) land(seq + (uint32_t)chunks - 2);
+            if (ok && chunks) land(seq + (uint32_t)chunks - 1);
             seq += (uint32_t)chunks;
         }
         if (invalid || bad) raise_status(PROM_ERR_BAD_WEIGHT);

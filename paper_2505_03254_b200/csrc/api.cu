@@ -2426,11 +2426,11 @@ static size_t workspace_bytes(long long m, int rank)
 template <class H, int R>
 static cudaError_t launch_inner(const Params &p, dim3 grid, cudaStream_t st)
 {
-    const cudaError_t e = raise_smem_limit(inner_tiles_kernel<H, R>, (int)inner_smem(kMaxRank));
+    const cudaError_t e = raise_smem_limit(inner_tiles_kernel<H, R>, (int)inner_smem(R, kMaxRank));
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];
-    fill_launch_cfg(cfg, attr, 1, kInnerThreads, inner_smem(p.pitch), st, true);
+    fill_launch_cfg(cfg, attr, 1, kInnerThreads, inner_smem(R, p.pitch), st, true);
     cfg.gridDim = grid;
     return cudaLaunchKernelEx(&cfg, inner_tiles_kernel<H, R>, p);
 }

@@ -332,16 +332,13 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torc
                         rstd: torch.Tensor, out=None, workspace: Optional[torch.Tensor] = None, stream=None):
     """prom_layer_norm_backward: dy and x [..., n], the forward pass's mean and rstd -> (dx like x, dweight, dbias
     [n] of weight's type, float32 without a weight); `out` may carry the three tensors, None for one that is not
-    wanted, dx being dy or x itself."""
-    n = x.shape[-1]
+    wanted, dx being dy or x itself.  Without a `workspace` (uint8) the call takes one from PyTorch's pool."""
     if out is None:
+        n = x.shape[-1]
         kept = torch.float32 if weight is None else weight.dtype
         out = (_empty(x.shape, x.dtype, x.device, stream), _empty((n,), kept, x.device, stream),
                _empty((n,), kept, x.device, stream))
     dx, dweight, dbias = out
-    if workspace is None and (dweight is not None or dbias is not None):
-        nbytes = layer_norm_backward_workspace_bytes(x.numel() // max(1, n), n)
-        workspace = _empty((nbytes,), torch.uint8, x.device, stream)
     _check((_native or native()).layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace,
                                                      _handle(stream)), "prom_layer_norm_backward")
     return dx, dweight, dbias
@@ -359,12 +356,10 @@ def pw_proj_adapters(x: torch.Tensor, batch: int, w_packed: torch.Tensor, cout: 
     """prom_pw_proj_adapters: x int8 [batch * rows_per_sample, cin], alpha float32 [cout], gamma_x float32 [batch],
     adapters a [n, rank, cin] and b [n, cout, rank] (bfloat16 or float16), scale float32 [n] or None, adapter_of_sample
     int32 [batch] (-1: none), all on the device -> y [batch * rows_per_sample, cout].  `y` may be given, a matrix of any
-    row pitch and of any of the three float types; otherwise it is made in `dtype`."""
+    row pitch and of any of the three float types; otherwise it is made in `dtype`.  Without a `workspace` (uint8) the call
+    takes one from PyTorch's pool."""
     if y is None:
         y = _empty((x.shape[0], cout), dtype, x.device, stream)
-    if workspace is None and a is not None and a.shape[0] and batch:
-        nbytes = pw_proj_adapters_workspace_bytes(batch, x.shape[0] // batch, a.shape[1])
-        workspace = _empty((nbytes,), torch.uint8, x.device, stream)
     _check((_native or native()).pw_proj_adapters(x, batch, w_packed, cout, alpha, gamma_x, a, b, scale, adapter_of_sample,
                                                   y, workspace, _handle(stream)), "prom_pw_proj_adapters")
     return y

@@ -111,6 +111,7 @@ __device__ __forceinline__ float outer(const Params &p, int a, int o, const floa
     const H *b = static_cast<const H *>(p.b) + ((size_t)a * p.cout + o) * p.rank;
     float s = 0.0f;
     if ((p.rank & 7) == 0) {
+#pragma unroll 4
         for (int j = 0; j < p.rank; j += 8) {
             const uint4 v = __ldg(reinterpret_cast<const uint4 *>(b + j));
             const float4 t0 = *reinterpret_cast<const float4 *>(t + j), t1 = *reinterpret_cast<const float4 *>(t + j + 4);
@@ -132,7 +133,9 @@ __device__ __forceinline__ float outer(const Params &p, int a, int o, const floa
 // ---- few rows: the projection -------------------------------------------------------------------------------
 // D[16 outputs][8 rows] += W[16][32] x[32][8] with the warp-level int8 MMA: the weights' bytes, a quarter of one per
 // product, are what has to be read, and with few rows the tensor memory path has nothing to amortise its set-up on.
-// A block takes 16 MO outputs and 8 MT rows, its eight warps share K in pieces of 256.
+// A block takes 16 MO outputs and 8 MT rows.  Latency is the bound, so its warps split K such that each has one piece of 64 PW
+// values (all of K at up to 4096 inputs) and every load of the call is on its way at once; with two pieces a warp
+// 32 rows 4096 -> 4096 took 8.0 us without adapters.
 // Codes become operands in three operations per 16: two's complement codes with the upper bit flipped are w + 2, and
 // (word >> 2 j) & 0x03030303 are the values k = j, 4 + j, 8 + j, 12 + j of the word's 16.  The rows' bytes are put in the same
 // order by transposing their 4 x 4 blocks, and 2 sum_k x is taken off at the end.
@@ -153,19 +156,18 @@ __device__ __forceinline__ void transpose_4x4(const uint4 &v, uint32_t (&o)[4])
     o[3] = __byte_perm(hi01, hi23, 0x7632);
 }
 
-constexpr int kRowWarps = 8;
-
-template <class H, class Y, int MO, int MT>
-__global__ void __launch_bounds__(32 * kRowWarps)
+// PW: words of 16 codes that a thread takes of each weight row.
+template <class H, class Y, int MO, int MT, int PW, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS)
 proj_rows_kernel(const Params p)
 {
-    __shared__ int acc_s[kRowWarps][16 * MO][8 * MT + 1];
-    __shared__ int sum_s[kRowWarps][8 * MT];
+    __shared__ int acc_s[8][16 * MO][8 * MT + 1];
+    __shared__ int sum_s[WARPS][8 * MT];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int o0 = blockIdx.x * 16 * MO;
     const long long r0 = (long long)blockIdx.y * 8 * MT;
     const int rowb = p.cin >> 2;
-    const bool wide = (rowb & 15) == 0;
+    const bool wide = rowb % (4 * PW) == 0;
     if (!p.chained) ptx::grid_dep_wait();
     ptx::grid_dep_launch();
 
@@ -179,9 +181,9 @@ proj_rows_kernel(const Params p)
             for (int e = 0; e < 4; ++e) d[o][i][e] = 0;
     }
     uint32_t invalid = 0;
-    for (int k0 = warp * 256; k0 < p.cin; k0 += 256 * kRowWarps) {
-        const int k = k0 + 64 * t;              // this thread's 64 of the piece
-        uint32_t w[MO][2][4];
+    for (int k0 = warp * 64 * PW; k0 < p.cin; k0 += 64 * PW * WARPS) {
+        const int k = k0 + 16 * PW * t;         // this thread's 16 PW of the piece
+        uint32_t w[MO][2][PW];
 #pragma unroll
         for (int o = 0; o < MO; ++o)
 #pragma unroll
@@ -189,23 +191,34 @@ proj_rows_kernel(const Params p)
                 const int row = o0 + 16 * o + 8 * h + g;
                 const uint8_t *src = p.w + (size_t)row * rowb + (k >> 2);
                 if (row < p.cout && wide && k < p.cin) {
-                    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(src));
-                    w[o][h][0] = v.x; w[o][h][1] = v.y; w[o][h][2] = v.z; w[o][h][3] = v.w;
+                    if constexpr (PW == 4) {
+                        const uint4 v = __ldg(reinterpret_cast<const uint4 *>(src));
+                        w[o][h][0] = v.x; w[o][h][1] = v.y; w[o][h][2] = v.z; w[o][h][3] = v.w;
+                    } else {
+                        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(src));
+                        w[o][h][0] = v.x; w[o][h][1] = v.y;
+                    }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < PW; ++i)
                         w[o][h][i] = row < p.cout && k + 16 * i < p.cin ? __ldg(reinterpret_cast<const uint32_t *>(src) + i) : 0u;
                 }
             }
+        uint4 v[MT][PW];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int c = 0; c < MT; ++c)
+#pragma unroll
+            for (int i = 0; i < PW; ++i) {
+                const long long r = r0 + 8 * c + g;
+                v[c][i] = make_uint4(0u, 0u, 0u, 0u);
+                if (r < p.m && k + 16 * i < p.cin) v[c][i] = __ldg(reinterpret_cast<const uint4 *>(p.x + r * p.cin + k + 16 * i));
+            }
+#pragma unroll
+        for (int i = 0; i < PW; ++i) {
             uint32_t b[MT][4];
 #pragma unroll
             for (int c = 0; c < MT; ++c) {
-                const long long r = r0 + 8 * c + g;
-                uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                if (r < p.m && k + 16 * i < p.cin) v = __ldg(reinterpret_cast<const uint4 *>(p.x + r * p.cin + k + 16 * i));
-                transpose_4x4(v, b[c]);
+                transpose_4x4(v[c][i], b[c]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sx[c] = __dp4a((int)b[c][j], 0x01010101, sx[c]);
             }
@@ -225,32 +238,66 @@ proj_rows_kernel(const Params p)
         }
     }
     if (invalid && blockIdx.y == 0) raise_status(PROM_ERR_BAD_WEIGHT);
+    // the warps' sums: those of the second eight first, added by the first eight to their own
+    auto put = [&](int slot) {
+#pragma unroll
+        for (int c = 0; c < MT; ++c)
+#pragma unroll
+            for (int o = 0; o < MO; ++o)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc_s[slot][16 * o + g + 8 * (e >> 1)][8 * c + 2 * t + (e & 1)] = d[o][c][e];
+    };
 #pragma unroll
     for (int c = 0; c < MT; ++c) {
         sx[c] += __shfl_xor_sync(0xFFFFFFFFu, sx[c], 1);
         sx[c] += __shfl_xor_sync(0xFFFFFFFFu, sx[c], 2);
         if (t == 0) sum_s[warp][8 * c + g] = sx[c];
-#pragma unroll
-        for (int o = 0; o < MO; ++o)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc_s[warp][16 * o + g + 8 * (e >> 1)][8 * c + 2 * t + (e & 1)] = d[o][c][e];
     }
+    if (WARPS > 8) {
+        if (warp >= 8) put(warp - 8);
+        __syncthreads();
+        if (warp < 8) {
+#pragma unroll
+            for (int c = 0; c < MT; ++c)
+#pragma unroll
+                for (int o = 0; o < MO; ++o)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) d[o][c][e] += acc_s[warp][16 * o + g + 8 * (e >> 1)][8 * c + 2 * t + (e & 1)];
+            __syncwarp();
+        }
+    }
+    if (warp < 8) put(warp);
     __syncthreads();
+    constexpr int kEach = (128 * MO * MT + 32 * WARPS - 1) / (32 * WARPS);      // outputs of a thread
+    float y[kEach], f[kEach];
+    int a[kEach];
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+        const int i = threadIdx.x + q * 32 * WARPS, o = i % (16 * MO), c = i / (16 * MO);
+        const long long r = r0 + c;
+        a[q] = -1;
+        y[q] = f[q] = 0.0f;
+        if (c >= 8 * MT || r >= p.m || o0 + o >= p.cout) continue;
+        int acc = 0, sum = 0;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) acc += acc_s[w][o][c];
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) sum += sum_s[w][c];
+        const int s = sample_of(p, r);
+        f[q] = row_factor(p, s);
+        y[q] = (float)(acc - 2 * sum) * __ldg(p.alpha + o0 + o) * f[q];
+        a[q] = adapter_of(p, s);
+        if (a[q] >= 0 && p.scale) f[q] *= __ldg(p.scale + a[q]);
+    }
     if (p.chained) ptx::grid_dep_wait();        // for the inner products
     bool bad = false;
-    for (int i = threadIdx.x; i < 16 * MO * 8 * MT; i += 32 * kRowWarps) {
-        const int o = i % (16 * MO), c = i / (16 * MO);
-        const long long r = r0 + c;
-        if (r >= p.m || o0 + o >= p.cout) continue;
-        int acc = 0;
 #pragma unroll
-        for (int w = 0; w < kRowWarps; ++w) acc += acc_s[w][o][c] - 2 * sum_s[w][c];
-        const int s = sample_of(p, r);
-        const float f = row_factor(p, s);
-        float y = (float)acc * __ldg(p.alpha + o0 + o) * f;
-        const int a = adapter_of(p, s);
-        if (a >= 0) y += (p.scale ? __ldg(p.scale + a) : 1.0f) * f * outer<H>(p, a, o0 + o, p.t + r * p.rank, bad);
-        static_cast<Y *>(p.y)[r * p.y_pitch + o0 + o] = norm::from_float<Y>(y);
+    for (int q = 0; q < kEach; ++q) {
+        const int i = threadIdx.x + q * 32 * WARPS, o = i % (16 * MO), c = i / (16 * MO);
+        const long long r = r0 + c;
+        if (c >= 8 * MT || r >= p.m || o0 + o >= p.cout) continue;
+        if (a[q] >= 0) y[q] += f[q] * outer<H>(p, a[q], o0 + o, p.t + r * p.rank, bad);
+        static_cast<Y *>(p.y)[r * p.y_pitch + o0 + o] = norm::from_float<Y>(y[q]);
     }
     if (bad) raise_status(PROM_ERR_BAD_WEIGHT);
 }

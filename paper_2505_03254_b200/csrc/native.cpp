@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -408,6 +409,37 @@ PyObject *layer_norm_i8(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// A call's workspace: the caller's tensor, or memory of PyTorch's pool that belongs to the stream the call runs on and goes
+// back to it when the call has been enqueued (what the stream is given next runs behind the call).
+class Workspace {
+public:
+    Workspace(PyObject *given, size_t bytes, void *st)
+    {
+        if (given != Py_None) {
+            const at::Tensor &t = dev(given, at::kByte, "workspace");
+            here(t, "workspace");
+            p = t.data_ptr();
+            size = (size_t)t.numel();
+        } else if (bytes) {
+            try {
+                p = own_ = c10::cuda::CUDACachingAllocator::raw_alloc_with_stream(bytes, static_cast<cudaStream_t>(st));
+            } catch (const std::exception &e) {
+                PyErr_SetString(PyExc_MemoryError, e.what());
+                throw ArgError();
+            }
+            size = bytes;
+        }
+    }
+    ~Workspace() { if (own_) c10::cuda::CUDACachingAllocator::raw_delete(own_); }
+    Workspace(const Workspace &) = delete;
+    Workspace &operator=(const Workspace &) = delete;
+    void *p = nullptr;
+    size_t size = 0;
+
+private:
+    void *own_ = nullptr;
+};
+
 // (dy, x, weight, mean, rstd, dx, dweight, dbias, workspace, stream)
 PyObject *layer_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -425,18 +457,11 @@ PyObject *layer_norm_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
         const auto *mean = static_cast<const float *>(vector(a[3], x.m, at::kFloat, "mean"));
         const auto *rstd = static_cast<const float *>(vector(a[4], x.m, at::kFloat, "rstd"));
         void *dw = vector(a[6], x.n, pts, "dweight"), *db = vector(a[7], x.n, pts, "dbias");
-        void *ws = nullptr;
-        size_t ws_bytes = 0;
-        if (a[8] != Py_None) {
-            const at::Tensor &t = dev(a[8], at::kByte, "workspace");
-            here(t, "workspace");
-            ws = t.data_ptr();
-            ws_bytes = (size_t)t.numel();
-        }
         void *st = stream(a[9]);
+        const Workspace ws(a[8], dw || db ? prom_layer_norm_backward_workspace_bytes(x.m, x.n) : 0, st);
         return call([&] {
             return prom_layer_norm_backward(dy.p, x.p, x.type, x.m, x.n, dy.pitch, x.pitch, w, pt, mean, rstd, dx.p, dx.pitch,
-                                            dw, db, ws, ws_bytes, st);
+                                            dw, db, ws.p, ws.size, st);
         });
     });
 }
@@ -481,20 +506,13 @@ PyObject *pw_proj_adapters(PyObject *, PyObject *const *a, Py_ssize_t n)
         }
         const Rows y = rows(a[10], "y");
         if (y.m != m || y.n != cout) fail(PyExc_ValueError, "%s must be [rows of x, cout]", "y");
-        void *ws = nullptr;
-        size_t ws_bytes = 0;
-        if (a[11] != Py_None) {
-            const at::Tensor &t = dev(a[11], at::kByte, "workspace");
-            here(t, "workspace");
-            ws = t.data_ptr();
-            ws_bytes = (size_t)t.numel();
-        }
         void *st = stream(a[12]);
+        const Workspace ws(a[11], ad.n ? prom_pw_proj_adapters_workspace_bytes(batch, batch ? m / batch : 1, ad.rank) : 0, st);
         const auto *xp = ptr<const int8_t>(x);
         const auto *wp = ptr<const uint8_t>(w);
         return call([&] {
             return prom_pw_proj_adapters(xp, batch, batch ? m / batch : 1, (int)cin, wp, cout, alpha, gamma, &ad, which, y.p,
-                                         y.type, y.pitch, ws, ws_bytes, st);
+                                         y.type, y.pitch, ws.p, ws.size, st);
         });
     });
 }

@@ -103,6 +103,24 @@ def test_matches_the_formula(shape, kind, out):
     _check(_call(c, dtype=out), c, shape)
 
 
+@pytest.mark.parametrize("mode", [1, 2])
+@pytest.mark.parametrize("shape", [(1, 1, 16, 8, 1, 1), (7, 1, 3008, 72, 3, 16), (9, 1, 1040, 136, 4, 20), (31, 1, 4096, 264, 9, 8), (70, 1, 2064, 4096, 5, 12),
+                                   (200, 1, 2048, 520, 40, 16), (300, 1, 976, 1288, 7, 64), (5, 70, 80, 328, 2, 33), (700, 1, 1536, 640, 90, 24)])
+def test_both_sets_of_kernels(shape, mode):
+    """Every shape runs on either; what the library's rule chooses is one of them."""
+    binding.debug_adapters(mode)
+    try:
+        for kind, out in ((torch.bfloat16, torch.bfloat16), (torch.float16, torch.float32)):
+            c = _case(sum(shape) + 1, *shape, kind=kind, order="mixed")
+            y = _call(c, dtype=out)
+            _check(y, c, shape)
+            assert torch.equal(y, _call(c, dtype=out))
+            c0 = {k: v for k, v in c.items() if k not in ("a", "b", "scale", "which")}
+            _check(_call(c0, dtype=out), c0, shape)
+    finally:
+        binding.debug_adapters()
+
+
 @pytest.mark.parametrize("batch", [1, 7, 40, 130, 700])
 def test_without_adapters(batch):
     for out in (torch.float32, torch.bfloat16, torch.float16):

@@ -357,18 +357,6 @@ template <> __device__ __forceinline__ void mma_16<__half>(float (&d)[4], const 
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <class H> __device__ __forceinline__ uint32_t pack_pair(float lo, float hi);
-template <> __device__ __forceinline__ uint32_t pack_pair<__nv_bfloat16>(float lo, float hi)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-template <> __device__ __forceinline__ uint32_t pack_pair<__half>(float lo, float hi)
-{
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-
 // The power of two by which a row's inner products are divided, so that the largest lies in [2^13, 2^14): far from both ends
 // of the 16-bit types.  1 for a row of (nearly) zeros or one that has a value which is not finite.
 __device__ __forceinline__ float row_power(float top, float &inverse)
@@ -592,7 +580,7 @@ inner_tiles_kernel(const Params p)
             for (int j = q; j < p.pitch / 2; j += 8) {
                 float lo = v[2 * j] * by, hi = v[2 * j + 1] * by;
                 for (int m = 0; m < p.terms; ++m) {
-                    out[m * (p.pitch / 2) + j] = pack_pair<H>(lo, hi);
+                    out[m * (p.pitch / 2) + j] = norm::pack_pair<H>(lo, hi);
                     lo -= norm::to_float(norm::from_float<H>(lo));
                     hi -= norm::to_float(norm::from_float<H>(hi));
                 }
@@ -989,8 +977,8 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
 #pragma unroll
                         for (int j = 0; j < 2; ++j)
                             *reinterpret_cast<uint4 *>(slab + tc::swz_offset((uint32_t)lane, (uint32_t)(h / 8 + j), 64u)) =
-                                make_uint4(pack_pair<Y>(y[8 * j], y[8 * j + 1]), pack_pair<Y>(y[8 * j + 2], y[8 * j + 3]),
-                                           pack_pair<Y>(y[8 * j + 4], y[8 * j + 5]), pack_pair<Y>(y[8 * j + 6], y[8 * j + 7]));
+                                make_uint4(norm::pack_pair<Y>(y[8 * j], y[8 * j + 1]), norm::pack_pair<Y>(y[8 * j + 2], y[8 * j + 3]),
+                                           norm::pack_pair<Y>(y[8 * j + 4], y[8 * j + 5]), norm::pack_pair<Y>(y[8 * j + 6], y[8 * j + 7]));
                     }
                 }
                 if (q.store) {

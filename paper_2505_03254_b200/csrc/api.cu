@@ -2241,27 +2241,86 @@ static prom_status launch(K *kernel, const P &p, long long grid, int threads, si
     return cuda_status(e);
 }
 
-// V accesses a thread: a warp per row up to 128 accesses, else the block that they fill.
-template <class T, int E, int V, bool CODES>
-static prom_status launch_forward(const Fwd &p, cudaStream_t st)
+// Rows after which the offset of a row from a 16-byte boundary repeats; 0 when the tensors' rows have different ones.
+static int period_of(size_t bytes, const void *x, int64_t x_pitch, const void *y, int64_t y_pitch, const void *z, int64_t z_pitch)
 {
-    const int pieces = p.n / E;
-    if (pieces <= 32 * V)
-        return launch(forward_kernel<T, E, V, CODES, true>, p, (p.m + 7) / 8, 256, 0, st);
-    return launch(forward_kernel<T, E, V, CODES, false>, p, p.m, (pieces + 32 * V - 1) / (32 * V) * 32, 0, st);
+    auto low = [&](const void *p, int64_t pitch, int row) { return (reinterpret_cast<uintptr_t>(p) + (uintptr_t)row * (uintptr_t)pitch * bytes) % 16; };
+    for (int row = 0; row < 2; ++row)
+        if ((y && low(y, y_pitch, row) != low(x, x_pitch, row)) || (z && low(z, z_pitch, row) != low(x, x_pitch, row))) return 0;
+    int p = 1;
+    while ((size_t)p * (size_t)(x_pitch % 16) * bytes % 16) p *= 2;
+    return p;
+}
+
+// How a block of up to `most` threads is shared out among groups for rows of `pieces` pieces; the grid that the rows fill.
+template <class P> static int share_out(P &p, int pieces, int most, const DeviceInfo &d)
+{
+    p.group = (pieces + 31) / 32 * 32;
+    p.groups = most / p.group;
+    // a group of several warps needs a named barrier, of which there are fifteen beside the block's
+    if (p.group > 32 && p.groups > 15) p.groups = 15;
+    // few rows: spread over the SMs before they share one
+    const long long each = (p.m + d.sms - 1) / d.sms;
+    if (each < p.groups) p.groups = (int)each;
+    const long long want = (p.m + p.groups - 1) / p.groups;
+    int blocks = (int)(want < d.sms ? want : d.sms);
+    // a group for every offset at least
+    while (blocks * p.groups < p.period) ++blocks;
+    return blocks;
+}
+
+template <class T, int E, int V, bool CODES>
+static prom_status launch_blocks(const Fwd &p, cudaStream_t st)
+{
+    return launch(forward_kernel<T, E, V, CODES>, p, p.m, (p.n / E + 32 * V - 1) / (32 * V) * 32, 0, st);
+}
+
+// As many warps as there is room for their rows, up to 32.
+template <class T, bool CODES>
+static int warps_for(const Fwd &p, const DeviceInfo &d)
+{
+    const size_t fit = ((size_t)d.smem_optin - 2048 - (size_t)p.n * 8) / ((size_t)p.n * sizeof(T));
+    return fit > 32 ? 32 : (int)fit;
+}
+template <class T, int V, bool CODES>
+static prom_status launch_short(const Fwd &p, const DeviceInfo &d, cudaStream_t st)
+{
+    return launch(forward_short_kernel<T, V, CODES>, p, d.sms, 1024, (size_t)p.n * 8, st);
 }
 
 template <class T, bool CODES>
-static prom_status run_forward(const Fwd &p, bool wide, cudaStream_t st)
+static prom_status launch_warps(const Fwd &p, int warps, const DeviceInfo &d, cudaStream_t st)
 {
+    if (raise_smem_limit(forward_warps_kernel<T, CODES>, d.smem_optin - 2048) != cudaSuccess) return PROM_ERR_CUDA;
+    return launch(forward_warps_kernel<T, CODES>, p, d.sms, 32 * warps, (size_t)p.n * (8 + warps * sizeof(T)), st);
+}
+
+template <class T, bool CODES>
+static prom_status run_forward(Fwd &p, bool wide, const DeviceInfo &d, cudaStream_t st)
+{
+    constexpr int E = kWide<T>;
+    // one more piece than the row fills, where it starts inside one
+    const int pieces = p.period ? (p.n + (p.period > 1 || !wide ? E - 1 : 0) + E - 1) / E : 0;
+    // Many rows: a warp each, out of registers up to 128 pieces (64 for codes), out of shared memory while about a dozen rows
+    // fit there (us, warps / blocks: 8192 x 4096 bf16 38 / 47, to codes 54 / 72; 4096 x 8192 bf16 53 / 38, to codes 71 / 63;
+    // 8192 x 4096 float32 61 / 49, to codes 64 / 95).
+    if (wide && p.m >= 8ll * d.sms) {
+        const int whole = p.n / E;
+        if (whole <= 32) return launch_short<T, 1, CODES>(p, d, st);
+        if (whole <= 64) return launch_short<T, 2, CODES>(p, d, st);
+        if (whole <= 128 && !CODES) return launch_short<T, 4, false>(p, d, st);
+        if (CODES ? p.n <= 4096 : whole <= 512) return launch_warps<T, CODES>(p, warps_for<T, CODES>(p, d), d, st);
+    }
+    if (p.period && pieces <= 1024 && !wide) {
+        const int blocks = share_out(p, pieces, 1024, d);
+        return launch(forward_groups_kernel<T, CODES>, p, blocks, p.group * p.groups, 0, st);
+    }
     if (wide) {
-        const int pieces = p.n / kWide<T>;
-        if (pieces <= 32) return launch_forward<T, kWide<T>, 1, CODES>(p, st);
-        if (pieces <= 64 || (pieces > 128 && pieces <= 2048)) return launch_forward<T, kWide<T>, 2, CODES>(p, st);
-        if (pieces <= 4096) return launch_forward<T, kWide<T>, 4, CODES>(p, st);
+        if (p.n / E <= 2048) return launch_blocks<T, E, 2, CODES>(p, st);
+        if (p.n / E <= 4096) return launch_blocks<T, E, 4, CODES>(p, st);
     } else {
-        if (p.n <= 128 || (p.n > 512 && p.n <= 4096)) return launch_forward<T, 1, 4, CODES>(p, st);
-        if (p.n <= 16384) return launch_forward<T, 1, 16, CODES>(p, st);
+        if (p.n <= 4096) return launch_blocks<T, 1, 4, CODES>(p, st);
+        if (p.n <= 16384) return launch_blocks<T, 1, 16, CODES>(p, st);
     }
     return launch(forward_long_kernel<T, CODES>, p, p.m, 1024, 0, st);
 }
@@ -2284,54 +2343,56 @@ static prom_status forward(const void *x, int type, int64_t m, int n, int64_t x_
     if (!aligned_to(mean, 4) || !aligned_to(rstd, 4)) return PROM_ERR_ALIGN;
     if (m == 0) return PROM_OK;
     if (!q && y == x && x_pitch != y_pitch && m > 1) return PROM_ERR_SHAPE;
+    if (m == 1) x_pitch = y_pitch = n;
     const size_t bytes = type_bytes(type);
     const bool wide = whole_pieces(x, x_pitch, bytes) && (q ? aligned_to(q, 8) : whole_pieces(y, y_pitch, bytes)) &&
                       (size_t)n * bytes % 16 == 0 && aligned16(w) && aligned16(b);
-    const Fwd p{x, m, x_pitch, y_pitch, n, {w, ptype}, {b, ptype}, eps, y, q, mean, rstd, gamma, scale};
-    if (type == PROM_TYPE_F32) return q ? run_forward<float, true>(p, wide, st) : run_forward<float, false>(p, wide, st);
+    Fwd p{x, m, x_pitch, y_pitch, n, {w, ptype}, {b, ptype}, eps, 0, 0, period_of(bytes, x, x_pitch, q ? nullptr : y, y_pitch, nullptr, 0),
+          y, q, mean, rstd, gamma, scale};
+    const DeviceInfo d = device_info();
+    if (!d.ok) return PROM_ERR_CUDA;
+    if (type == PROM_TYPE_F32) return q ? run_forward<float, true>(p, wide, d, st) : run_forward<float, false>(p, wide, d, st);
     if (type == PROM_TYPE_BF16)
-        return q ? run_forward<__nv_bfloat16, true>(p, wide, st) : run_forward<__nv_bfloat16, false>(p, wide, st);
-    return q ? run_forward<__half, true>(p, wide, st) : run_forward<__half, false>(p, wide, st);
+        return q ? run_forward<__nv_bfloat16, true>(p, wide, d, st) : run_forward<__nv_bfloat16, false>(p, wide, d, st);
+    return q ? run_forward<__half, true>(p, wide, d, st) : run_forward<__half, false>(p, wide, d, st);
 }
 
 template <class T, int E, int V, bool RING>
-static prom_status launch_backward(Bwd &p, const DeviceInfo &d, int &blocks, cudaStream_t st)
+static prom_status launch_backward(Bwd &p, int pieces, const DeviceInfo &d, int &blocks, cudaStream_t st)
 {
-    const int pieces = p.n / E;
-    p.group = (pieces + 32 * V - 1) / (32 * V) * 32;
-    p.groups = kBwdThreads<E, V> / p.group;
-    // few rows: spread over the SMs before they share one
-    const long long each = (p.m + d.sms - 1) / d.sms;
-    if (each < p.groups) p.groups = (int)each;
-    const long long want = (p.m + p.groups - 1) / p.groups;
-    blocks = (int)(want < d.sms ? want : d.sms);
+    blocks = share_out(p, (pieces + V - 1) / V, kBwdThreads<E, V>, d);
     p.stages = 0;
     size_t smem = p.part ? (size_t)2 * p.n_pad * 4 : 0;
+    constexpr int kRoom = 10240;        // static shared memory and what the system keeps
     if (RING) {
-        // rows in flight: as many as fit, up to eight a group
-        const size_t stage = (size_t)2 * p.n * sizeof(T) * p.groups;
-        const size_t room = (size_t)d.smem_optin - 4096;
+        // rows in flight: as many as fit, but a whole number of steps
+        const size_t stage = (size_t)2 * p.n * sizeof(T) * p.groups, room = (size_t)d.smem_optin - kRoom;
         p.stages = (int)(room / stage < (size_t)kMaxStages ? room / stage : (size_t)kMaxStages);
         if (p.stages > p.group) p.stages = p.group;
         const size_t bytes = stage * p.stages;
         if (bytes > smem) smem = bytes;
     }
-    if (raise_smem_limit(backward_kernel<T, E, V, RING>, d.smem_optin - 4096) != cudaSuccess) return PROM_ERR_CUDA;
+    if (raise_smem_limit(backward_kernel<T, E, V, RING>, d.smem_optin - kRoom) != cudaSuccess) return PROM_ERR_CUDA;
     return launch(backward_kernel<T, E, V, RING>, p, blocks, p.group * p.groups, smem, st);
 }
 
 template <class T>
 static prom_status run_backward(Bwd &p, bool wide, const DeviceInfo &d, int &blocks, cudaStream_t st)
 {
+    constexpr int E = kWide<T>;
+    const int pieces = p.n / E, period = p.period;
+    const int shifted = period ? (p.n + (period > 1 || !wide ? E - 1 : 0) + E - 1) / E : 0;
+    // rows of less than a kilobyte come by plain loads too: a bulk copy each costs more than it moves
+    if (period && shifted <= (wide ? 64 : 1024)) return launch_backward<T, E, 1, false>(p, shifted, d, blocks, st);
+    p.period = 1;
     if (wide) {
-        constexpr int E = kWide<T>;
-        const int pieces = p.n / E;
-        if (pieces <= 32) return launch_backward<T, E, 1, true>(p, d, blocks, st);
-        if (pieces <= 64 * (kBwdThreads<E, 2> / 32)) return launch_backward<T, E, 2, true>(p, d, blocks, st);
-        if (pieces <= 128 * (kBwdThreads<E, 4> / 32)) return launch_backward<T, E, 4, true>(p, d, blocks, st);
+        if (pieces <= 1024) return launch_backward<T, E, 1, true>(p, pieces, d, blocks, st);
+        if (pieces <= 2 * kBwdThreads<E, 2>) return launch_backward<T, E, 2, true>(p, pieces, d, blocks, st);
+        if (pieces <= 4 * kBwdThreads<E, 4>) return launch_backward<T, E, 4, true>(p, pieces, d, blocks, st);
     } else {
-        if (p.n <= 4 * kBwdThreads<1, 4>) return launch_backward<T, 1, 4, false>(p, d, blocks, st);
-        if (p.n <= 16 * kBwdThreads<1, 16>) return launch_backward<T, 1, 16, false>(p, d, blocks, st);
+        if (p.n <= 1024) return launch_backward<T, 1, 1, false>(p, p.n, d, blocks, st);
+        if (p.n <= 4 * kBwdThreads<1, 4>) return launch_backward<T, 1, 4, false>(p, p.n, d, blocks, st);
+        if (p.n <= 16 * kBwdThreads<1, 16>) return launch_backward<T, 1, 16, false>(p, p.n, d, blocks, st);
     }
     // the column sums first: dx may be dy or x
     if (p.part) {
@@ -2351,7 +2412,8 @@ static prom_status run_backward(Bwd &p, bool wide, const DeviceInfo &d, int &blo
 
 static size_t backward_workspace(int64_t m, int n, int sms)
 {
-    return (size_t)(m < sms ? m : sms) * 2 * (size_t)((n + 3) & ~3) * sizeof(float);
+    // (up to eight blocks where there are fewer rows: one for every offset of a row from a 16-byte boundary)
+    return (size_t)(m < 8 ? 8 : (m < sms ? m : sms)) * 2 * (size_t)((n + 3) & ~3) * sizeof(float);
 }
 
 }}  // namespace prom::norm
@@ -2907,6 +2969,7 @@ prom_status prom_layer_norm_backward(const void *dy_dev, const void *x_dev, prom
         ++g_launches;
         return cuda_status(e);
     }
+    if (m == 1) dy_pitch = x_pitch = dx_pitch = n;
     norm::Bwd p;
     memset(&p, 0, sizeof(p));
     p.dy = dy_dev; p.x = x_dev; p.m = m; p.dy_pitch = dy_pitch; p.x_pitch = x_pitch; p.dx_pitch = dx_pitch; p.n = n;
@@ -2918,6 +2981,7 @@ prom_status prom_layer_norm_backward(const void *dy_dev, const void *x_dev, prom
     const bool wide = norm::whole_pieces(x_dev, x_pitch, bytes) && norm::whole_pieces(dy_dev, dy_pitch, bytes) &&
                       (!dx_dev || norm::whole_pieces(dx_dev, dx_pitch, bytes)) && (size_t)n * bytes % 16 == 0 &&
                       aligned16(weight_dev);
+    p.period = norm::period_of(bytes, x_dev, x_pitch, dy_dev, dy_pitch, dx_dev, dx_pitch);
     int blocks = 0;
     if (type == PROM_TYPE_F32) s = norm::run_backward<float>(p, wide, d, blocks, st);
     else if (type == PROM_TYPE_BF16) s = norm::run_backward<__nv_bfloat16>(p, wide, d, blocks, st);

@@ -5,17 +5,25 @@
 //     gamma = max |y|,  scale = 127 / max(gamma, 1e-5),  q = clip(round(y scale), -128, 127)      (as in actquant.cuh)
 // All three are bound by their bytes: x is read once and a row's statistics are taken from the registers that hold it.
 //
-// Forward: a warp takes a row of up to 128 accesses of 16 bytes, a block a longer one, up to four accesses a thread; the loads
-// of a row are in flight together and several rows share an SM.  Statistics in binary32, the variance from the
-// differences to the mean (a sum of squares would cancel).  For codes the statistics are taken in binary64 and
-// rounded once, and every step behind them is a single binary32 operation, so that a code does not depend on the
-// order of a sum.
+// Threads come in groups that share a row, a 16-byte piece (8 or 4 columns) each, as many groups as fill an SM, and walk over
+// the rows: what belongs to a column (weight, bias, the sums for dw and db) stays in registers, and the next rows are on
+// their way while the current ones are worked on.  Two rows are taken at a time where registers allow, so that an exchange
+// between the warps of a group serves both.  (A warp or block per row, with the parameters read again for each, spent its
+// time on those reads: 16384 x 4096 bf16 77 us forward.)
 //
-// Backward: one block per SM walks over its rows, in groups of threads that each take a row at a time.  A row of x
-// and dy comes through a ring of bulk copies, a few rows ahead, and the column sums dw and db stay in registers
-// until the block has seen its last row: one partial sum per block, added up by a second kernel in a fixed order
-// (no atomics: the same inputs give the same bits).  Rows that are not made of whole 16-byte pieces are read element
-// by element, and rows too long for the registers take plain loops.
+// Rows need not start on a 16-byte boundary.  A thread's piece is one of memory, its columns are shifted by the row's offset,
+// and a group only takes rows of one offset (it repeats after at most eight rows), so the shifted parameters stay in
+// registers too; only the first and the last piece of a row are read and written by the element.
+//
+// Forward: statistics in binary32, the variance from the differences to the mean (a sum of squares would cancel).  For
+// codes the statistics are taken in binary64 and rounded once, and every step behind them is a single binary32 operation, so
+// that a code does not depend on the order of a sum.
+//
+// Backward: rows of a kilobyte or more on 16-byte boundaries come through a ring of bulk copies.  The column sums make one
+// partial sum per block, added up by a second kernel in a fixed order (no atomics: the same inputs give the same bits).
+//
+// Rows of more than 1024 pieces take several pieces a thread, very long ones plain loops; tensors whose rows have different
+// offsets are read element by element.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -32,30 +40,98 @@ namespace prom { namespace norm {
 // ---- values of the three types, E to an access: 16 bytes, or one element -------------------------
 template <class T> __device__ __forceinline__ float to_float(T v);
 template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 v)
+{
+    return __uint_as_float((uint32_t)__bfloat16_as_ushort(v) << 16);
+}
 template <> __device__ __forceinline__ float to_float<__half>(__half v) { return __half2float(v); }
 template <class T> __device__ __forceinline__ T from_float(float v);
 template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 
+// Two values to one word, and one of a word's two.  Shifts and packed conversions: a 16-bit value converted alone takes the
+// pipe of the special functions, at an eighth of their rate, which was the bound of every kernel here.
+template <class T> __device__ __forceinline__ uint32_t pack_pair(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack_pair<__nv_bfloat16>(float lo, float hi)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+template <> __device__ __forceinline__ uint32_t pack_pair<__half>(float lo, float hi)
+{
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+template <class T> __device__ __forceinline__ float half_of(uint32_t w, int upper);
+template <> __device__ __forceinline__ float half_of<__nv_bfloat16>(uint32_t w, int upper) { return __uint_as_float(upper ? w & 0xFFFF0000u : w << 16); }
+template <> __device__ __forceinline__ float half_of<__half>(uint32_t w, int upper)
+{
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+    return upper ? f.y : f.x;
+}
+template <> __device__ __forceinline__ float half_of<float>(uint32_t w, int) { return __uint_as_float(w); }      // (not used)
+
 template <class T> constexpr int kWide = 16 / (int)sizeof(T);      // elements of a 16-byte access
 
 template <class T, int E> struct Piece {
-    union { uint4 raw; T v[kWide<T>]; };
+    uint4 raw;
     __device__ __forceinline__ Piece() : raw(make_uint4(0u, 0u, 0u, 0u)) {}
     __device__ __forceinline__ void load(const T *p) { raw = *reinterpret_cast<const uint4 *>(p); }
     __device__ __forceinline__ void store(T *p) const { *reinterpret_cast<uint4 *>(p) = raw; }
-    __device__ __forceinline__ float get(int e) const { return to_float<T>(v[e]); }
-    __device__ __forceinline__ void set(int e, float f) { v[e] = from_float<T>(f); }
+    __device__ __forceinline__ float get(int e) const
+    {
+        const int i = sizeof(T) == 4 ? e : e >> 1;
+        const uint32_t w = i == 0 ? raw.x : i == 1 ? raw.y : i == 2 ? raw.z : raw.w;
+        return sizeof(T) == 4 ? __uint_as_float(w) : half_of<T>(w, e & 1);
+    }
+    __device__ __forceinline__ void set(const float (&f)[E])
+    {
+        if constexpr (sizeof(T) == 4) raw = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+        else raw = make_uint4(pack_pair<T>(f[0], f[1]), pack_pair<T>(f[2], f[3]), pack_pair<T>(f[4 % E], f[5 % E]), pack_pair<T>(f[6 % E], f[7 % E]));
+    }
+    // From here on the values are converted again instead of being kept as floats, twice the registers of 16-bit ones.
+    __device__ __forceinline__ void again() { asm volatile("" : "+r"(raw.x), "+r"(raw.y), "+r"(raw.z), "+r"(raw.w)); }
 };
+// The piece of columns c .. c + E - 1 of a row of n, of which some may lie outside it.
+template <class T, int E> __device__ __forceinline__ void load_at(Piece<T, E> &v, const T *row, int c, int n)
+{
+    if (c >= 0 && c + E <= n) {
+        v.load(row + c);
+    } else {
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (c + e >= 0 && c + e < n) {
+                if constexpr (sizeof(T) == 4) w[e] = __float_as_uint((float)row[c + e]);
+                else w[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[c + e] << (16 * (e & 1));
+            }
+        v.raw = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+template <class T, int E> __device__ __forceinline__ void store_at(const Piece<T, E> &v, T *row, int c, int n)
+{
+    if (c >= 0 && c + E <= n) {
+        v.store(row + c);
+    } else {
+        const uint32_t w[4] = {v.raw.x, v.raw.y, v.raw.z, v.raw.w};
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (c + e >= 0 && c + e < n) {
+                if constexpr (sizeof(T) == 4) row[c + e] = __uint_as_float(w[e]);
+                else reinterpret_cast<uint16_t *>(row)[c + e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+            }
+    }
+}
 template <class T> struct Piece<T, 1> {
     T v;
     __device__ __forceinline__ Piece() : v(from_float<T>(0.0f)) {}
     __device__ __forceinline__ void load(const T *p) { v = *p; }
     __device__ __forceinline__ void store(T *p) const { *p = v; }
     __device__ __forceinline__ float get(int) const { return to_float<T>(v); }
-    __device__ __forceinline__ void set(int, float f) { v = from_float<T>(f); }
+    __device__ __forceinline__ void set(const float (&f)[1]) { v = from_float<T>(f[0]); }
+    __device__ __forceinline__ void again() {}
 };
 
 // A vector of parameters (weight or bias) of any of the types; absent: `otherwise`.
@@ -68,6 +144,16 @@ struct Vector {
         if (type == PROM_TYPE_F32) return __ldg(static_cast<const float *>(p) + i);
         if (type == PROM_TYPE_BF16) return to_float(__ldg(static_cast<const __nv_bfloat16 *>(p) + i));
         return to_float(__ldg(static_cast<const __half *>(p) + i));
+    }
+    // E neighbours from column c on, which may start and end outside the n; once per thread
+    template <int E> __device__ __forceinline__ void get_at(int c, int n, float otherwise, float (&f)[E]) const
+    {
+        if (c % E == 0 && c >= 0 && c + E <= n && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
+            get<E>(c, otherwise, f);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) f[e] = c + e >= 0 && c + e < n ? at(c + e, otherwise) : 0.0f;
+        }
     }
     // E neighbours from a multiple of E; the base is 16-byte aligned
     template <int E> __device__ __forceinline__ void get(int i, float otherwise, float (&f)[E]) const
@@ -112,11 +198,30 @@ struct Fwd {
     int n;
     Vector w, b;
     double eps;
+    int group, groups, period;      // as in Bwd
     void *y;                // nullptr for codes
     int8_t *q;              // [m][n]
     float *mean, *rstd;     // may be nullptr
     float *gamma, *scale;   // with q
 };
+
+// A value as a double without a conversion (a quarter of the rate of the arithmetic): the bits moved into a double's places
+// are the value times 2^-896, zeros and subnormals included, and the factor enters the next multiply-add.  What is not finite
+// would become finite: the callers look for it.
+template <class T> __device__ __forceinline__ double scaled_down(float f)
+{
+    const int u = __float_as_int(f);
+    return __hiloint2double((u >> 3) & (int)0x8FFFFFFF, std::is_same<T, float>::value ? u << 29 : 0);   // (16-bit types end above)
+}
+__device__ __forceinline__ double two_896() { return __hiloint2double(0x77F00000, 0); }
+
+// 1 / sqrt(v): the approximation and one step of Newton's method.
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const float r = rsqrtf(v);
+    return v > 0.0f && v < 1e38f ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
+}
+__device__ __forceinline__ double inverse_root(double v) { return rsqrt(v); }
 
 // ---- sums over the threads that share a row --------------------------------------------------------
 template <class A> __device__ __forceinline__ A warp_sum(A v)
@@ -126,7 +231,12 @@ template <class A> __device__ __forceinline__ A warp_sum(A v)
     return v;
 }
 // Maxima that keep a NaN: a row with one has no codes that mean anything, and its gamma says so.
-__device__ __forceinline__ float max_nan(float a, float b) { return b > a || b != b ? b : a; }
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 __device__ __forceinline__ float warp_max(float v)
 {
 #pragma unroll
@@ -173,20 +283,482 @@ template <int E> __device__ __forceinline__ void store_codes(int8_t *q, const fl
     }
 }
 
-// ---- forward: the row in registers ------------------------------------------------------------------
-// WARP: a warp per row, else a block.  V accesses of E elements a thread, thread t takes accesses t, t + threads, ...
-template <class T, int E, int V, bool CODES, bool WARP>
-__global__ void __launch_bounds__(WARP ? 256 : 1024)
+// ---- groups of threads that share rows -----------------------------------------------------------------
+__device__ __forceinline__ void group_barrier(int g, int threads)
+{
+    if (threads == (int)blockDim.x) __syncthreads();
+    else ptx::named_sync(1u + (uint32_t)g, (uint32_t)threads);
+}
+
+// The sums over a warp of four values at once: lane bit 4 chooses between the first and the second two, bit 3 within them.
+__device__ __forceinline__ float warp_sum_4(float a, float b, float c, float d)
+{
+    const int lane = threadIdx.x & 31;
+    const bool up = (lane & 16) != 0;
+    float x = up ? c : a, y = up ? d : b;
+    x += __shfl_xor_sync(0xFFFFFFFFu, up ? a : c, 16);
+    y += __shfl_xor_sync(0xFFFFFFFFu, up ? b : d, 16);
+    const bool second = (lane & 8) != 0;
+    float v = second ? y : x;
+    v += __shfl_xor_sync(0xFFFFFFFFu, second ? x : y, 8);
+#pragma unroll
+    for (int k = 4; k > 0; k >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, k);
+    return v;
+}
+__device__ __forceinline__ void spread_4(float v, float &a, float &b, float &c, float &d)
+{
+    a = __shfl_sync(0xFFFFFFFFu, v, 0);
+    b = __shfl_sync(0xFFFFFFFFu, v, 8);
+    c = __shfl_sync(0xFFFFFFFFu, v, 16);
+    d = __shfl_sync(0xFFFFFFFFu, v, 24);
+}
+
+// The same for two values: lane bit 4 chooses.
+template <class A> __device__ __forceinline__ A warp_sum_2(A a, A b)
+{
+    const bool up = (threadIdx.x & 16) != 0;
+    A v = up ? b : a;
+    v += __shfl_xor_sync(0xFFFFFFFFu, up ? a : b, 16);
+#pragma unroll
+    for (int k = 8; k > 0; k >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, k);
+    return v;
+}
+__device__ __forceinline__ float warp_max_2(float a, float b)
+{
+    const bool up = (threadIdx.x & 16) != 0;
+    float v = max_nan(up ? b : a, __shfl_xor_sync(0xFFFFFFFFu, up ? a : b, 16));
+#pragma unroll
+    for (int k = 8; k > 0; k >>= 1) v = max_nan(v, __shfl_xor_sync(0xFFFFFFFFu, v, k));
+    return v;
+}
+// Two sums (or maxima) over a group: the first in the lower half of every warp, the second in the upper one, where what
+// follows from them is worked out for both at once.  `red` has a pair per warp of the block and is free again behind the
+// barrier after next.
+template <class A> __device__ __forceinline__ A group_sum_2(A a, A b, A (*red)[2], int g, int threads)
+{
+    A v = warp_sum_2(a, b);
+    const int lane = threadIdx.x & 31, warps = threads >> 5;
+    if (warps > 1) {
+        if ((lane & 15) == 0) red[threadIdx.x >> 5][lane >> 4] = v;
+        group_barrier(g, threads);
+        A x = (A)0, y = (A)0;
+        if (lane < warps) { x = red[g * warps + lane][0]; y = red[g * warps + lane][1]; }
+        v = warp_sum_2(x, y);
+    }
+    return v;
+}
+__device__ __forceinline__ float group_max_2(float a, float b, float (*red)[2], int g, int threads)
+{
+    float v = warp_max_2(a, b);
+    const int lane = threadIdx.x & 31, warps = threads >> 5;
+    if (warps > 1) {
+        if ((lane & 15) == 0) red[threadIdx.x >> 5][lane >> 4] = v;
+        group_barrier(g, threads);
+        float x = 0.0f, y = 0.0f;
+        if (lane < warps) { x = red[g * warps + lane][0]; y = red[g * warps + lane][1]; }
+        v = warp_max_2(x, y);
+    }
+    return v;
+}
+template <class A> __device__ __forceinline__ void spread_2(A v, A (&to)[2])
+{
+    to[0] = __shfl_sync(0xFFFFFFFFu, v, 0);
+    to[1] = __shfl_sync(0xFFFFFFFFu, v, 16);
+}
+
+// The parameters as floats in shared memory, a piece's first and last four columns apart, so that a warp's 16-byte accesses
+// are side by side.  n is a multiple of E.
+template <int E> __device__ __forceinline__ void stage_parameters(const Fwd &p, float *sw, float *sb)
+{
+    const int pieces = p.n / E;
+    for (int i = threadIdx.x; i < p.n; i += blockDim.x) {
+        const int at = ((i % E / 4) * pieces + i / E) * 4 + i % 4;
+        sw[at] = p.w.at(i, 1.0f);
+        sb[at] = p.b.at(i, 0.0f);
+    }
+}
+template <int E>
+__device__ __forceinline__ void parameters_of(const float *sw, const float *sb, int pieces, int piece, float (&w)[E], float (&b)[E])
+{
+#pragma unroll
+    for (int f = 0; f < E / 4; ++f) {
+        const float4 a = reinterpret_cast<const float4 *>(sw)[f * pieces + piece], c = reinterpret_cast<const float4 *>(sb)[f * pieces + piece];
+        w[4 * f] = a.x; w[4 * f + 1] = a.y; w[4 * f + 2] = a.z; w[4 * f + 3] = a.w;
+        b[4 * f] = c.x; b[4 * f + 1] = c.y; b[4 * f + 2] = c.z; b[4 * f + 3] = c.w;
+    }
+}
+
+// Columns that the first piece of the row at `p` has before it.
+template <class T> __device__ __forceinline__ int offset_of(const void *p) { return (int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T)); }
+
+// ---- forward: groups ----------------------------------------------------------------------------------
+template <class T, bool CODES>
+__global__ void __launch_bounds__(1024, 1)
+forward_groups_kernel(const Fwd p)
+{
+    using Sum = typename std::conditional<CODES, double, float>::type;
+    constexpr int E = kWide<T>;
+    __shared__ Sum red_mean[32][2], red_var[32][2];
+    __shared__ float red_max[32][2];
+    const int g = (int)threadIdx.x / p.group, t = (int)threadIdx.x - g * p.group, n = p.n;
+    const int all = (int)gridDim.x * p.groups / p.period * p.period;       // groups: a whole number for every offset
+    const int r0 = g * (int)gridDim.x + (int)blockIdx.x, m = (int)p.m;     // (the last rows go round the SMs)
+    ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
+    if (r0 >= all || r0 >= m) return;           // (whole groups, which meet no other's threads)
+    const T *x = static_cast<const T *>(p.x);
+    const int c = t * E - offset_of<T>(x + r0 * p.x_pitch);
+    const bool full = c >= 0 && c + E <= n, some = c + E > 0 && c < n;
+    float w[E], b[E];
+    p.w.get_at<E>(c, n, 1.0f, w);
+    p.b.get_at<E>(c, n, 0.0f, b);
+    const Sum inv_n = (Sum)1 / (Sum)n;
+    // codes of a whole piece in one store
+    const bool wide_q = CODES && (reinterpret_cast<uintptr_t>(p.q) + (uint64_t)((long long)r0 * n + c)) % E == 0 && (long long)all * n % E == 0;
+
+    Piece<T, E> v[2], next[2];
+    auto load = [&](int r, Piece<T, E> &to) {
+        to.raw = make_uint4(0u, 0u, 0u, 0u);
+        if (r < m && some) load_at<T, E>(to, x + (long long)r * p.x_pitch, c, n);
+    };
+    load(r0, next[0]);
+    load(all < m - r0 ? r0 + all : m, next[1]);
+#pragma unroll 1
+    for (long long rr = r0; rr < m; rr += 2ll * all) {
+        const int r = (int)rr;
+        const bool two = (long long)r + all < m;
+        v[0] = next[0];
+        v[1] = next[1];
+        load(rr + 2ll * all < m ? (int)(rr + 2ll * all) : m, next[0]);
+        load(rr + 3ll * all < m ? (int)(rr + 3ll * all) : m, next[1]);
+        Sum s[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            s[k] = 0;
+            if constexpr (CODES) {
+                float odd = 0.0f;               // NaN once a value is not finite
+#pragma unroll
+                for (int e = 0; e < E; ++e) {   // (what lies outside the row is zero)
+                    const float f = v[k].get(e);
+                    s[k] = fma(scaled_down<T>(f), two_896(), s[k]);
+                    odd = fmaf(f, 0.0f, odd);
+                }
+                s[k] += (double)odd;
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[k] += v[k].get(e);
+            }
+        }
+        Sum mean[2];
+        spread_2(group_sum_2(s[0], s[1], red_mean, g, p.group) * inv_n, mean);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            s[k] = 0;
+            v[k].again();
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                Sum d;
+                if constexpr (CODES) d = fma(scaled_down<T>(v[k].get(e)), two_896(), -mean[k]);
+                else d = v[k].get(e) - mean[k];
+                if (full || (c + e >= 0 && c + e < n)) s[k] = fma(d, d, s[k]);
+            }
+        }
+        const float rstd_half = (float)inverse_root(group_sum_2(s[0], s[1], red_var, g, p.group) * inv_n + (Sum)p.eps);
+        const float mu[2] = {(float)mean[0], (float)mean[1]};
+        float rstd[2];
+        spread_2(rstd_half, rstd);
+        if (t == 0) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                if (k == 0 || two) {
+                    if (p.mean) p.mean[r + k * all] = mu[k];
+                    if (p.rstd) p.rstd[r + k * all] = rstd[k];
+                }
+        }
+        if constexpr (!CODES) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if ((k && !two) || !some) continue;
+                v[k].again();
+                float f[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) f[e] = (v[k].get(e) - mu[k]) * rstd[k] * w[e] + b[e];
+                Piece<T, E> o;
+                o.set(f);
+                store_at<T, E>(o, static_cast<T *>(p.y) + (long long)(r + k * all) * p.y_pitch, c, n);
+            }
+        } else {
+            float top[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                top[k] = 0.0f;
+                v[k].again();
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (full || (c + e >= 0 && c + e < n)) top[k] = max_nan(top[k], fabsf(affine_exact(v[k].get(e), mu[k], rstd[k], w[e], b[e])));
+            }
+            const float top_half = group_max_2(top[0], top[1], red_max, g, p.group);
+            float scale[2];
+            spread_2(top_half, top);
+            spread_2(actq::scale_of(top_half, 1e-5f), scale);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if (k && !two) continue;
+                const float sc = scale[k];
+                if (t == 0) { p.gamma[r + k * all] = top[k]; p.scale[r + k * all] = sc; }
+                if (!some) continue;
+                v[k].again();                   // computed again: kept, the values would take more registers than there are
+                float f[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) f[e] = affine_exact(v[k].get(e), mu[k], rstd[k], w[e], b[e]);
+                int8_t *out = p.q + (long long)(r + k * all) * n + c;
+                if (full && wide_q) {
+                    store_codes<E>(out, f, sc);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (c + e >= 0 && c + e < n) out[e] = actq::quantise_one(f[e], sc);
+                }
+            }
+        }
+    }
+}
+
+// ---- forward: a warp per short row ----------------------------------------------------------------------------
+// V pieces a lane, in registers; the parameters in shared memory as in the next kernel.  (A bulk copy of a row of a
+// kilobyte costs more than its loads: 25088 x 192 float32, 14.3 us through shared memory, 11.5 here.)
+template <class T, int V, bool CODES>
+__global__ void __launch_bounds__(1024, 1)
+forward_short_kernel(const Fwd p)
+{
+    using Sum = typename std::conditional<CODES, double, float>::type;
+    constexpr int E = kWide<T>;
+    extern __shared__ __align__(16) float short_params[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = p.n, m = (int)p.m, pieces = n / E;
+    float *sw = short_params, *sb = short_params + n;
+    ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
+    stage_parameters<E>(p, sw, sb);
+    __syncthreads();
+    const Sum inv_n = (Sum)1 / (Sum)n;
+#pragma unroll 1
+    for (long long r = (long long)warp * gridDim.x + blockIdx.x; r < m; r += 32ll * gridDim.x) {
+        const T *row = static_cast<const T *>(p.x) + r * p.x_pitch;
+        Piece<T, E> v[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (lane + 32 * i < pieces) v[i].load(row + (lane + 32 * i) * E);
+        Sum s = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {   // (what lies past the row is zero)
+                if constexpr (CODES) s = fma(scaled_down<T>(v[i].get(e)), two_896(), s);
+                else s += v[i].get(e);
+            }
+        const Sum mean = warp_sum(s) * inv_n;
+        s = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (lane + 32 * i < pieces) {
+                v[i].again();
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    Sum d;
+                    if constexpr (CODES) d = fma(scaled_down<T>(v[i].get(e)), two_896(), -mean);
+                    else d = v[i].get(e) - mean;
+                    s = fma(d, d, s);
+                }
+            }
+        float mu = (float)mean, rstd = (float)inverse_root(warp_sum(s) * inv_n + (Sum)p.eps);
+        if constexpr (!CODES) {
+            T *out = static_cast<T *>(p.y) + r * p.y_pitch;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (lane + 32 * i < pieces) {
+                    float w[E], b[E];
+                    parameters_of<E>(sw, sb, pieces, lane + 32 * i, w, b);
+                    v[i].again();
+#pragma unroll
+                    for (int e = 0; e < E; ++e) w[e] = (v[i].get(e) - mu) * rstd * w[e] + b[e];
+                    v[i].set(w);
+                    v[i].store(out + (lane + 32 * i) * E);
+                }
+        } else {
+            float y[V][E], top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (lane + 32 * i < pieces) {
+                    float w[E], b[E];
+                    parameters_of<E>(sw, sb, pieces, lane + 32 * i, w, b);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        y[i][e] = affine_exact(v[i].get(e), mu, rstd, w[e], b[e]);
+                        top = max_nan(top, fabsf(y[i][e]));
+                    }
+                }
+            top = warp_max(top);
+            const float sc = actq::scale_of(top, 1e-5f);
+            if (lane == 0) { p.gamma[r] = top; p.scale[r] = sc; }
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (lane + 32 * i < pieces) store_codes<E>(p.q + r * n + (lane + 32 * i) * E, y[i], sc);
+            if (!(top <= 3.402823466e38f)) mu = rstd = __int_as_float(0x7FC00000);      // (as in the next kernel)
+        }
+        if (lane == 0) {
+            if (p.mean) p.mean[r] = mu;
+            if (p.rstd) p.rstd[r] = rstd;
+        }
+    }
+}
+
+// ---- forward: a warp per row ------------------------------------------------------------------------------
+// For many rows of whole pieces.  No exchange between warps, and what belongs to a row worked out once for all of it.  A bulk
+// copy brings the row into shared memory, where the warp passes over it three times (four for codes): in registers the
+// longer rows leave none for the arithmetic.  As many warps as there is room for rows; while one waits for its row the
+// others work.
+template <class T, bool CODES>
+__global__ void __launch_bounds__(1024, 1)
+forward_warps_kernel(const Fwd p)
+{
+    using Sum = typename std::conditional<CODES, double, float>::type;
+    constexpr int E = kWide<T>;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(8) uint64_t bars[32];
+    __shared__ volatile int failed;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = p.n, m = (int)p.m, pieces = n / E;
+    const int own = (int)blockDim.x >> 5, warps = (int)gridDim.x * own;
+    const uint32_t row_bytes = (uint32_t)n * (uint32_t)sizeof(T);
+    float *sw = reinterpret_cast<float *>(smem), *sb = sw + n;      // (n is a multiple of E: both 16-byte aligned)
+    const uint4 *mine = reinterpret_cast<const uint4 *>(smem + (size_t)n * 8 + (size_t)warp * row_bytes);
+    const uint32_t mine_addr = ptx::smem_u32(mine), bar = ptx::smem_u32(bars) + 8u * warp;
+    if (lane == 0) { ptx::mbar_init(bar, 1); ptx::mbar_init_fence(); }
+    if (threadIdx.x == 0) failed = 0;
+    ptx::grid_dep_wait();
+    ptx::grid_dep_launch();
+    const T *x = static_cast<const T *>(p.x);
+    auto fetch = [&](long long r) {
+        ptx::mbar_expect_tx(bar, row_bytes);
+        ptx::bulk_load(mine_addr, x + r * p.x_pitch, row_bytes, bar);
+    };
+    long long r = (long long)warp * gridDim.x + blockIdx.x;        // (the last rows go round the SMs)
+    if (lane == 0 && r < m) fetch(r);
+    stage_parameters<E>(p, sw, sb);
+    __syncthreads();
+    auto parameters = [&](int piece, float (&w)[E], float (&b)[E]) { parameters_of<E>(sw, sb, pieces, piece, w, b); };
+    const Sum inv_n = (Sum)1 / (Sum)n;
+    uint32_t phase = 0;
+#pragma unroll 1
+    for (; r < m; r += warps, phase ^= 1u) {
+        if (!ptx::mbar_try_wait(bar, phase)) {
+            const unsigned long long t0 = ptx::globaltimer();
+            while (!ptx::mbar_try_wait(bar, phase))
+                if (failed || ptx::globaltimer() - t0 > actq::kWaitLimitNs) { failed = 1; break; }
+        }
+        if (__any_sync(0xFFFFFFFFu, failed)) break;
+        Piece<T, E> v;
+        Sum s = 0, s2 = 0;
+#pragma unroll 4
+        for (int i = lane; i < pieces; i += 32) {
+            v.raw = mine[i];
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                if constexpr (CODES) {
+                    s = fma(scaled_down<T>(v.get(e)), two_896(), s);
+                    s2 = fma(scaled_down<T>(v.get(e + 1)), two_896(), s2);
+                } else {
+                    s += v.get(e);
+                    s2 += v.get(e + 1);
+                }
+            }
+        }
+        const Sum mean = warp_sum(s + s2) * inv_n;
+        s = s2 = 0;
+#pragma unroll 4
+        for (int i = lane; i < pieces; i += 32) {
+            v.raw = mine[i];
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                Sum d, d2;
+                if constexpr (CODES) {
+                    d = fma(scaled_down<T>(v.get(e)), two_896(), -mean);
+                    d2 = fma(scaled_down<T>(v.get(e + 1)), two_896(), -mean);
+                } else {
+                    d = v.get(e) - mean;
+                    d2 = v.get(e + 1) - mean;
+                }
+                s = fma(d, d, s);
+                s2 = fma(d2, d2, s2);
+            }
+        }
+        float mu = (float)mean, rstd = (float)inverse_root(warp_sum(s + s2) * inv_n + (Sum)p.eps);
+        if constexpr (!CODES) {
+            T *out = static_cast<T *>(p.y) + r * p.y_pitch;
+#pragma unroll 2
+            for (int i = lane; i < pieces; i += 32) {
+                float w[E], b[E];
+                parameters(i, w, b);
+                v.raw = mine[i];
+#pragma unroll
+                for (int e = 0; e < E; ++e) w[e] = (v.get(e) - mu) * rstd * w[e] + b[e];
+                v.set(w);
+                v.store(out + i * E);
+            }
+        } else {
+            float top = 0.0f;
+#pragma unroll 2
+            for (int i = lane; i < pieces; i += 32) {
+                float w[E], b[E];
+                parameters(i, w, b);
+                v.raw = mine[i];
+#pragma unroll
+                for (int e = 0; e < E; ++e) top = max_nan(top, fabsf(affine_exact(v.get(e), mu, rstd, w[e], b[e])));
+            }
+            top = warp_max(top);
+            const float sc = actq::scale_of(top, 1e-5f);
+            if (lane == 0) { p.gamma[r] = top; p.scale[r] = sc; }
+            int8_t *out = p.q + r * n;
+#pragma unroll 2
+            for (int i = lane; i < pieces; i += 32) {
+                float w[E], b[E];
+                parameters(i, w, b);
+                v.raw = mine[i];
+#pragma unroll
+                for (int e = 0; e < E; ++e) w[e] = affine_exact(v.get(e), mu, rstd, w[e], b[e]);
+                store_codes<E>(out + i * E, w, sc);
+            }
+            // (a value that is not finite shows in the maximum only: the sums took its bits for a number's)
+            if (!(top <= 3.402823466e38f)) mu = rstd = __int_as_float(0x7FC00000);
+        }
+        if (lane == 0) {
+            if (p.mean) p.mean[r] = mu;
+            if (p.rstd) p.rstd[r] = rstd;
+        }
+        __syncwarp();                           // the row has been read
+        if (lane == 0 && r + warps < m) fetch(r + warps);
+    }
+    __syncthreads();
+    if (failed) {
+        // copies may be in flight yet: outwait them before the shared memory goes
+        const unsigned long long t0 = ptx::globaltimer();
+        while (ptx::globaltimer() - t0 < actq::kWaitLimitNs) {}
+        if (threadIdx.x == 0) raise_status(PROM_ERR_TIMEOUT);
+    }
+}
+
+// ---- forward: a block per row ---------------------------------------------------------------------------
+// V accesses of E elements a thread, thread t takes accesses t, t + threads, ...
+template <class T, int E, int V, bool CODES>
+__global__ void __launch_bounds__(1024)
 forward_kernel(const Fwd p)
 {
     using Sum = typename std::conditional<CODES, double, float>::type;
     __shared__ Sum red[2][32];
     __shared__ float red_max[32];
-    const int threads = WARP ? 32 : (int)blockDim.x, t = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x;
-    const long long r = WARP ? (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : (long long)blockIdx.x;
+    const int threads = (int)blockDim.x, t = (int)threadIdx.x;
+    const long long r = blockIdx.x;
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
-    if (r >= p.m) return;               // whole warps; blocks have exactly their rows
     const int pieces = p.n / E;
     const T *row = static_cast<const T *>(p.x) + r * p.x_pitch;
     Piece<T, E> v[V];
@@ -195,23 +767,36 @@ forward_kernel(const Fwd p)
         if (t + i * threads < pieces) v[i].load(row + (size_t)(t + i * threads) * E);
 
     Sum s = 0;
+    float odd = 0.0f;                   // NaN once a value is not finite
 #pragma unroll
     for (int i = 0; i < V; ++i)
 #pragma unroll
-        for (int e = 0; e < E; ++e) s += (Sum)v[i].get(e);          // what lies past the row is zero
-    if constexpr (WARP) s = warp_sum(s); else s = block_sum(s, red[0]);
+        for (int e = 0; e < E; ++e) {   // (what lies past the row is zero)
+            const float f = v[i].get(e);
+            if constexpr (CODES) {
+                s = fma(scaled_down<T>(f), two_896(), s);
+                odd = fmaf(f, 0.0f, odd);
+            } else {
+                s += f;
+            }
+        }
+    if constexpr (CODES) s += (double)odd;
+    s = block_sum(s, red[0]);
     const Sum mean = s / (Sum)p.n;
     s = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i)
         if (t + i * threads < pieces) {
+            v[i].again();
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const Sum d = (Sum)v[i].get(e) - mean;
-                s += d * d;
+                Sum d;
+                if constexpr (CODES) d = fma(scaled_down<T>(v[i].get(e)), two_896(), -mean);
+                else d = v[i].get(e) - mean;
+                s = fma(d, d, s);
             }
         }
-    if constexpr (WARP) s = warp_sum(s); else s = block_sum(s, red[1]);
+    s = block_sum(s, red[1]);
     float rstd;
     if constexpr (CODES) rstd = (float)(1.0 / sqrt(s / (double)p.n + p.eps));
     else rstd = 1.0f / sqrtf(s / (float)p.n + (float)p.eps);
@@ -225,38 +810,58 @@ forward_kernel(const Fwd p)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int c = (t + i * threads) * E;
-            if (t + i * threads >= pieces) break;
-            float w[E], b[E];
-            p.w.get<E>(c, 1.0f, w);
-            p.b.get<E>(c, 0.0f, b);
-            Piece<T, E> o;
+            if (t + i * threads < pieces) {
+                float w[E], b[E];
+                p.w.get<E>(c, 1.0f, w);
+                p.b.get<E>(c, 0.0f, b);
+                v[i].again();
 #pragma unroll
-            for (int e = 0; e < E; ++e) o.set(e, (v[i].get(e) - mu) * rstd * w[e] + b[e]);
-            o.store(out + c);
+                for (int e = 0; e < E; ++e) w[e] = (v[i].get(e) - mu) * rstd * w[e] + b[e];
+                Piece<T, E> o;
+                o.set(w);
+                o.store(out + c);
+            }
         }
     } else {
-        float y[V][E], top = 0.0f;
+        // few values a thread are kept between the maximum and the codes, many are computed again
+        constexpr bool kKeep = V * E <= 16;
+        float y[kKeep ? V : 1][E], top = 0.0f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int c = (t + i * threads) * E;
-            if (t + i * threads >= pieces) break;
-            float w[E], b[E];
-            p.w.get<E>(c, 1.0f, w);
-            p.b.get<E>(c, 0.0f, b);
+            if (t + i * threads < pieces) {
+                float w[E], b[E];
+                p.w.get<E>(c, 1.0f, w);
+                p.b.get<E>(c, 0.0f, b);
+                v[i].again();
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                y[i][e] = affine_exact(v[i].get(e), mu, rstd, w[e], b[e]);
-                top = max_nan(top, fabsf(y[i][e]));
+                for (int e = 0; e < E; ++e) {
+                    const float f = affine_exact(v[i].get(e), mu, rstd, w[e], b[e]);
+                    if constexpr (kKeep) y[i][e] = f;
+                    top = max_nan(top, fabsf(f));
+                }
             }
         }
-        if constexpr (WARP) top = warp_max(top); else top = block_max(top, red_max);
+        top = block_max(top, red_max);
         const float sc = actq::scale_of(top, 1e-5f);
         if (t == 0) { p.gamma[r] = top; p.scale[r] = sc; }
         int8_t *out = p.q + r * p.n;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            if (t + i * threads >= pieces) break;
-            store_codes<E>(out + (size_t)(t + i * threads) * E, y[i], sc);
+            const int c = (t + i * threads) * E;
+            if (t + i * threads < pieces) {
+                if constexpr (kKeep) {
+                    store_codes<E>(out + c, y[i], sc);
+                } else {
+                    float w[E], b[E], f[E];
+                    p.w.get<E>(c, 1.0f, w);
+                    p.b.get<E>(c, 0.0f, b);
+                    v[i].again();
+#pragma unroll
+                    for (int e = 0; e < E; ++e) f[e] = affine_exact(v[i].get(e), mu, rstd, w[e], b[e]);
+                    store_codes<E>(out + c, f, sc);
+                }
+            }
         }
     }
 }
@@ -318,16 +923,16 @@ struct Bwd {
     int n_pad;              // n rounded up to a multiple of 4
     int group;              // threads that share a row
     int groups;             // of them in a block
+    int period;             // rows after which the offset from a 16-byte boundary repeats
     int stages;             // rows of each group's ring
 };
 
-// Threads of a block, by the registers that a thread's columns take (2 V E sums, and the weights where they fit beside).
-template <int E, int V> constexpr bool kHeavy = V * E >= 32 || V >= 16;
-template <int E, int V> constexpr int kBwdThreads = kHeavy<E, V> ? 512 : 768;
-constexpr int kMaxGroups = 768 / 32;
-constexpr int kMaxStages = 8;
-
-__device__ __forceinline__ void group_barrier(int g, int threads) { ptx::named_sync(1u + (uint32_t)g, (uint32_t)threads); }
+constexpr int kMaxGroups = 32;
+constexpr int kMaxStages = 16;              // rows of a group's ring
+// One piece a thread (up to 1024 to a row): as many threads as an SM has; two rows at a time out of the ring, one with the next
+// one on its way without it.  More: fewer threads, for their column sums are registers (2 V E of them).
+template <int E, int V> constexpr int kBwdThreads = V * E >= 32 || V >= 16 ? 512 : (V * E > 8 ? 768 : 1024);
+template <int V, bool RING> constexpr int kBwdRows = V == 1 && RING ? 2 : 1;
 
 // RING: rows come through shared memory by bulk copies (whole 16-byte pieces), else by plain loads.
 // Shared memory: the rings ([groups][stages][2][row bytes]), used again at the end for the groups' column sums.
@@ -335,18 +940,24 @@ template <class T, int E, int V, bool RING>
 __global__ void __launch_bounds__(kBwdThreads<E, V>, 1)
 backward_kernel(const Bwd p)
 {
+    constexpr int R = kBwdRows<V, RING>;
+    constexpr bool kShift = !RING && V == 1 && E > 1;       // rows may start anywhere
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t bars[kMaxGroups * kMaxStages];
-    __shared__ float2 red[2][kMaxGroups];
+    __shared__ __align__(8) uint64_t bars[RING ? kMaxGroups * kMaxStages : 1];
+    __shared__ float4 red[2][32];
     __shared__ volatile int failed;
     const int g = (int)threadIdx.x / p.group, t = (int)threadIdx.x - g * p.group;
     const int lane = threadIdx.x & 31, warps = p.group >> 5, first_warp = g * warps;
-    const int pieces = p.n / E;
-    const uint32_t row_bytes = (uint32_t)p.n * (uint32_t)sizeof(T);
+    const int n = p.n, pieces = n / E;
+    const uint32_t row_bytes = (uint32_t)n * (uint32_t)sizeof(T);
     const uint32_t ring = ptx::smem_u32(smem) + (uint32_t)g * p.stages * 2u * row_bytes;
     const uint32_t bar0 = ptx::smem_u32(bars) + 8u * (uint32_t)(g * p.stages);
-    const long long step = (long long)gridDim.x * p.groups, r0 = (long long)blockIdx.x * p.groups + g;
+    const long long step = (long long)((int)gridDim.x * p.groups / p.period * p.period);
+    const long long first = (long long)g * gridDim.x + blockIdx.x, r0 = first < step ? first : p.m;     // (the last rows go round the SMs)
     const T *x = static_cast<const T *>(p.x), *dy = static_cast<const T *>(p.dy);
+    const int c0 = kShift ? t * E - (r0 < p.m ? offset_of<T>(x + r0 * p.x_pitch) : 0) : 0;
+    // whether access i of this thread is in the row
+    auto in_row = [&](int i) { return kShift ? c0 + E > 0 && c0 < n : t + i * p.group < pieces; };
 
     if (RING) {
         if (t < p.stages) ptx::mbar_init(bar0 + 8u * t, 1);
@@ -365,11 +976,12 @@ backward_kernel(const Bwd p)
     if (RING && t == 0)
         for (int s = 0; s < p.stages && ahead < p.m; ++s, ahead += step) fetch(s, ahead);
 
-    constexpr bool kHoldW = !kHeavy<E, V>;
+    constexpr bool kHoldW = V * E < 16;
     float held[kHoldW ? V : 1][E], dw[V][E], db[V][E];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        if constexpr (kHoldW)
+        if constexpr (kShift) p.w.get_at<E>(c0, n, 1.0f, held[0]);
+        else if constexpr (kHoldW)
             if (t + i * p.group < pieces) p.w.get<E>((t + i * p.group) * E, 1.0f, held[i]);
 #pragma unroll
         for (int e = 0; e < E; ++e) dw[i][e] = db[i][e] = 0.0f;
@@ -377,81 +989,136 @@ backward_kernel(const Bwd p)
     const float inv_n = 1.0f / (float)p.n;
     int s = 0, which = 0;
     uint32_t phase = 0;
-    for (long long r = r0; r < p.m; r += step) {
-        const float mean = __ldg(p.mean + r), rstd = __ldg(p.rstd + r);
-        Piece<T, E> vx[V], vd[V];
-        if constexpr (RING) {
-            // A wait that runs out is the last one: the block goes on without waiting, so that its barriers stay in
-            // step, fetches nothing more and reports at the end.
-            const unsigned long long t0 = ptx::globaltimer();
-            while (!ptx::mbar_try_wait(bar0 + 8u * s, phase))
-                if (failed || ptx::globaltimer() - t0 > actq::kWaitLimitNs) { failed = 1; break; }
-            const T *sx = reinterpret_cast<const T *>(smem + (size_t)(g * p.stages + s) * 2 * row_bytes);
-            const T *sd = reinterpret_cast<const T *>(smem + (size_t)(g * p.stages + s) * 2 * row_bytes + row_bytes);
+    float next_mean[R], next_rstd[R];           // of the rows behind the current ones: not waited for
+    auto statistics = [&](long long r) {
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (t + i * p.group < pieces) {
-                    vx[i].load(sx + (size_t)(t + i * p.group) * E);
-                    vd[i].load(sd + (size_t)(t + i * p.group) * E);
-                }
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (t + i * p.group < pieces) {
-                    vx[i].load(x + r * p.x_pitch + (size_t)(t + i * p.group) * E);
-                    vd[i].load(dy + r * p.dy_pitch + (size_t)(t + i * p.group) * E);
-                }
+        for (int k = 0; k < R; ++k) {
+            const long long rk = r + k * step;
+            next_mean[k] = rk < p.m ? __ldg(p.mean + rk) : 0.0f;
+            next_rstd[k] = rk < p.m ? __ldg(p.rstd + rk) : 0.0f;
         }
-        float2 sum = make_float2(0.0f, 0.0f);       // of g and of g xh
+    };
+    statistics(r0);
+    Piece<T, E> next_x[RING ? 1 : V], next_d[RING ? 1 : V];
+    auto load = [&](long long r) {
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (t + i * p.group < pieces) {
-                float w[E];
-                if constexpr (!kHoldW) p.w.get<E>((t + i * p.group) * E, 1.0f, w);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float we = kHoldW ? held[kHoldW ? i : 0][e] : w[e];
-                    const float d = vd[i].get(e), xh = (vx[i].get(e) - mean) * rstd, gr = d * we;
-                    sum.x += gr;
-                    sum.y += gr * xh;
-                    dw[i][e] += d * xh;
-                    db[i][e] += d;
+        for (int i = 0; i < (RING ? 1 : V); ++i)
+            if (r < p.m && in_row(i)) {
+                const T *xr = x + r * p.x_pitch, *dr = dy + r * p.dy_pitch;
+                if constexpr (kShift) {
+                    load_at<T, E>(next_x[i], xr, c0, n);
+                    load_at<T, E>(next_d[i], dr, c0, n);
+                } else {
+                    next_x[i].load(xr + (size_t)(t + i * p.group) * E);
+                    next_d[i].load(dr + (size_t)(t + i * p.group) * E);
                 }
             }
-        sum.x = warp_sum(sum.x);
-        sum.y = warp_sum(sum.y);
-        if (warps > 1) {
-            if (lane == 0) red[which][threadIdx.x >> 5] = sum;
-            group_barrier(g, p.group);
-            // every thread of the group has read its part of the stage, so it can be filled again
-            float2 a = lane < warps ? red[which][first_warp + lane] : make_float2(0.0f, 0.0f);
-            sum.x = warp_sum(a.x);
-            sum.y = warp_sum(a.y);
-            which ^= 1;                         // the next row's sums go elsewhere: these may still be read
-        } else {
-            __syncwarp();
+    };
+    if constexpr (!RING) load(r0);
+#pragma unroll 1
+    for (long long r = r0; r < p.m; r += R * step) {
+        float mean[R], rstd[R], s1[R], s2[R];   // sums of g and of g xh
+        Piece<T, E> vx[R][V], vd[R][V];
+#pragma unroll
+        for (int k = 0; k < R; ++k) { mean[k] = next_mean[k]; rstd[k] = next_rstd[k]; }
+        statistics(r + R * step);
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const long long rk = r + k * step;
+            const bool there = rk < p.m;
+            if constexpr (RING) {
+                if (there) {
+                    // A wait that runs out is the last one: the block goes on without waiting, so that its barriers stay in
+                    // step, fetches nothing more and reports at the end.
+                    const int st = s + k < p.stages ? s + k : s + k - p.stages;
+                    const uint32_t ph = s + k < p.stages ? phase : phase ^ 1u;
+                    if (!ptx::mbar_try_wait(bar0 + 8u * st, ph)) {
+                        const unsigned long long t0 = ptx::globaltimer();
+                        while (!ptx::mbar_try_wait(bar0 + 8u * st, ph))
+                            if (failed || ptx::globaltimer() - t0 > actq::kWaitLimitNs) { failed = 1; break; }
+                    }
+                    const T *sx = reinterpret_cast<const T *>(smem + (size_t)(g * p.stages + st) * 2 * row_bytes);
+                    const T *sd = reinterpret_cast<const T *>(smem + (size_t)(g * p.stages + st) * 2 * row_bytes + row_bytes);
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        if (t + i * p.group < pieces) {
+                            vx[k][i].load(sx + (size_t)(t + i * p.group) * E);
+                            vd[k][i].load(sd + (size_t)(t + i * p.group) * E);
+                        }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) { vx[k][i] = next_x[RING ? 0 : i]; vd[k][i] = next_d[RING ? 0 : i]; }
+                load(r + step);
+            }
         }
-        if (RING) {
-            if (t == 0 && ahead < p.m && !failed) { fetch(s, ahead); ahead += step; }
-            if (++s == p.stages) { s = 0; phase ^= 1u; }
-        }
-        if (p.dx) {
-            const float c1 = sum.x * inv_n, c2 = sum.y * inv_n;
-            T *out = static_cast<T *>(p.dx) + r * p.dx_pitch;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            s1[k] = s2[k] = 0.0f;
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (t + i * p.group < pieces) {
-                    Piece<T, E> o;
+                if (in_row(i)) {
                     float w[E];
                     if constexpr (!kHoldW) p.w.get<E>((t + i * p.group) * E, 1.0f, w);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
+                    for (int e = 0; e < E; ++e) {       // (a row that is not there is one of zeros, as is dy outside a row)
                         const float we = kHoldW ? held[kHoldW ? i : 0][e] : w[e];
-                        const float xh = (vx[i].get(e) - mean) * rstd;
-                        o.set(e, rstd * (vd[i].get(e) * we - c1 - xh * c2));
+                        const float d = vd[k][i].get(e), xh = (vx[k][i].get(e) - mean[k]) * rstd[k], gr = d * we;
+                        s1[k] += gr;
+                        s2[k] += gr * xh;
+                        dw[i][e] += d * xh;
+                        db[i][e] += d;
                     }
-                    o.store(out + (size_t)(t + i * p.group) * E);
                 }
+        }
+        float v = R == 2 ? warp_sum_4(s1[0], s2[0], s1[R - 1], s2[R - 1]) : warp_sum_4(s1[0], s2[0], 0.0f, 0.0f);
+        if (warps > 1) {
+            if ((lane & 7) == 0) reinterpret_cast<float *>(&red[which][threadIdx.x >> 5])[lane >> 3] = v;
+            group_barrier(g, p.group);
+            // every thread of the group has read its part of the stages, so they can be filled again
+            const float4 a = lane < warps ? red[which][first_warp + lane] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            v = warp_sum_4(a.x, a.y, a.z, a.w);
+            which ^= 1;                         // the next rows' sums go elsewhere: these may still be read
+        } else {
+            __syncwarp();
+        }
+        float unused1, unused2;
+        if constexpr (R == 2) spread_4(v, s1[0], s2[0], s1[R - 1], s2[R - 1]);
+        else spread_4(v, s1[0], s2[0], unused1, unused2);
+        if (RING) {
+            if (t == 0 && !failed) {
+#pragma unroll
+                for (int k = 0; k < R; ++k)
+                    if (ahead < p.m) { fetch(s + k < p.stages ? s + k : s + k - p.stages, ahead); ahead += step; }
+            }
+            s += R;
+            if (s >= p.stages) { s -= p.stages; phase ^= 1u; }
+        }
+        if (p.dx) {
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                const long long rk = r + k * step;
+                const float c1 = s1[k] * inv_n, c2 = s2[k] * inv_n;
+                T *out = static_cast<T *>(p.dx) + rk * p.dx_pitch;
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (rk < p.m && in_row(i)) {
+                        float w[E];
+                        if constexpr (!kHoldW) p.w.get<E>((t + i * p.group) * E, 1.0f, w);
+                        vx[k][i].again();
+                        vd[k][i].again();
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            const float we = kHoldW ? held[kHoldW ? i : 0][e] : w[e];
+                            const float xh = (vx[k][i].get(e) - mean[k]) * rstd[k];
+                            w[e] = rstd[k] * (vd[k][i].get(e) * we - c1 - xh * c2);
+                        }
+                        Piece<T, E> o;
+                        o.set(w);
+                        if constexpr (kShift) store_at<T, E>(o, out, c0, n);
+                        else o.store(out + (size_t)(t + i * p.group) * E);
+                    }
+            }
         }
     }
     __syncthreads();
@@ -466,24 +1133,26 @@ backward_kernel(const Bwd p)
 
     // The groups' column sums, added in the order of the groups; all copies have landed and been read.
     float *acc = reinterpret_cast<float *>(smem);       // [2][n_pad]
+    for (int c = threadIdx.x; c < 2 * p.n_pad; c += blockDim.x) acc[c] = 0.0f;
+    __syncthreads();
     for (int k = 0; k < p.groups; ++k) {
         if (g == k) {
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (t + i * p.group < pieces) {
-                    const int c = (t + i * p.group) * E;
+                if (in_row(i)) {
+                    const int c = kShift ? c0 : (t + i * p.group) * E;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        acc[c + e] = dw[i][e] + (k ? acc[c + e] : 0.0f);
-                        acc[p.n_pad + c + e] = db[i][e] + (k ? acc[p.n_pad + c + e] : 0.0f);
-                    }
+                    for (int e = 0; e < E; ++e)
+                        if (!kShift || (c + e >= 0 && c + e < n)) {
+                            acc[c + e] += dw[i][e];
+                            acc[p.n_pad + c + e] += db[i][e];
+                        }
                 }
         }
         __syncthreads();
     }
     float *mine = p.part + (size_t)blockIdx.x * 2 * p.n_pad;
-    for (int c = threadIdx.x; c < 2 * p.n_pad; c += blockDim.x)
-        mine[c] = c % p.n_pad < p.n ? acc[c] : 0.0f;
+    for (int c = threadIdx.x; c < 2 * p.n_pad; c += blockDim.x) mine[c] = acc[c];
 }
 
 // Rows of any length: dx by a block per row, and the column sums of a slice of rows by a block per 256 columns.

@@ -172,7 +172,8 @@ def test_row_pitches(n, pitch, dtype):
     out.check("y")
     assert bool((out.view(m, pitch)[:, n:] == 3.0).all())
     # dense results from the same rows, and the backward pass
-    assert torch.equal(binding.layer_norm(x, w, b, EPS)[0], y)
+    # (within the same bound, not bit for bit: where a row starts decides which thread adds which of its values)
+    _near(binding.layer_norm(x, w, b, EPS)[0], want, _slack(x.double(), mu, rs, w), "dense y")
     assert torch.equal(binding.layer_norm_i8(x, w, b, EPS)[0], binding.layer_norm_i8(x.contiguous(), w, b, EPS)[0])
     dy = torch.randn((m, n), device="cuda").to(dtype)
     res = Guarded(m * pitch * size, dtype=dtype, fill=3.0)
@@ -185,6 +186,52 @@ def test_row_pitches(n, pitch, dtype):
     slack = 64 * U * (dy.double().abs().sum(0) * 30)
     assert bool(((dense[0].double() - dx.double()).abs() <= torch.finfo(dtype).eps * dense[0].double().abs() + 1e-4).all())
     assert bool(((dense[1].double() - dw.double()).abs() <= slack).all()) and bool(((dense[2].double() - db.double()).abs() <= slack).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n", [(1, 5), (7, 3), (9, 17), (40, 95), (300, 97), (1201, 129), (500, 1003), (150, 2049), (40, 4093), (20, 8185), (20, 8200)])
+@pytest.mark.parametrize("shift", [0, 2, 5])
+def test_rows_that_start_anywhere(m, n, dtype, shift):
+    """Dense rows of odd widths, from a base inside a 16-byte piece: nothing outside the rows is read into a result or written."""
+    size = torch.finfo(dtype).bits // 8
+    x0, w, b = _inputs(m + n + shift, m, n, dtype, torch.float32)
+    flat = torch.full((m * n + 16,), float("nan"), dtype=dtype, device="cuda")
+    x = flat[shift:shift + m * n].view(m, n)
+    x.copy_(x0)
+    want, mu, rs, _ = _definition(x, w, b)
+    out = Guarded((m * n + 16) * size, dtype=dtype, fill=3.0)
+    y = out.t[shift:shift + m * n].view(m, n)
+    _, mean, rstd = binding.layer_norm(x, w, b, EPS, out=(y, torch.empty(m, device="cuda"), torch.empty(m, device="cuda")))
+    out.check("y")
+    assert bool((out.t[:shift] == 3.0).all()) and bool((out.t[shift + m * n:] == 3.0).all())
+    _near(y, want, _slack(x.double(), mu, rs, w), "y")
+    q, gamma, scale = binding.layer_norm_i8(x, w, b, EPS)
+    wide = torch.zeros((m, (n + 15) // 16 * 16), dtype=dtype, device="cuda")
+    wide[:, :n] = x
+    ref = binding.layer_norm_i8(wide[:, :n], w, b, EPS)
+    assert torch.equal(q, ref[0]) and torch.equal(gamma, ref[1]) and torch.equal(scale, ref[2])
+    dflat = torch.full((m * n + 16,), float("nan"), dtype=dtype, device="cuda")
+    dy = dflat[shift:shift + m * n].view(m, n)
+    dy.copy_(torch.randn((m, n), device="cuda"))
+    res = Guarded((m * n + 16) * size, dtype=dtype, fill=3.0)
+    dx = res.t[shift:shift + m * n].view(m, n)
+    dw, db = torch.empty_like(w), torch.empty_like(b)
+    binding.layer_norm_backward(dy, x, w, mean, rstd, out=(dx, dw, db))
+    res.check("dx")
+    assert bool((res.t[:shift] == 3.0).all()) and bool((res.t[shift + m * n:] == 3.0).all())
+    xh = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    gd = dy.double() * w.double()
+    top = xh.abs().amax(1, keepdim=True) + 1 + mean.double().abs()[:, None] * rstd.double()[:, None]
+    want = rstd.double()[:, None] * (gd - gd.mean(1, keepdim=True) - xh * (gd * xh).mean(1, keepdim=True))
+    _near(dx, want, 256 * U * rstd.double()[:, None] * gd.abs().amax(1, keepdim=True) * top * top, "dx")
+    _near(dw, (dy.double() * xh).sum(0), 256 * U * (dy.double().abs() * top).sum(0), "dweight")
+    _near(db, dy.double().sum(0), 256 * U * dy.double().abs().sum(0), "dbias")
+    # tensors whose rows have different offsets
+    if m > 1:
+        plain = binding.layer_norm(x, w, b, EPS, out=(torch.empty((m, n + 1), dtype=dtype, device="cuda")[:, :n], None, None))[0]
+        _near(plain, _definition(x, w, b)[0], _slack(x.double(), mu, rs, w), "y")
+        other = binding.layer_norm_backward(dy.clone(), x, w, mean, rstd)
+        _near(other[0], want, 256 * U * rstd.double()[:, None] * gd.abs().amax(1, keepdim=True) * top * top, "dx")
 
 
 @pytest.mark.parametrize("shift", [1, 3])

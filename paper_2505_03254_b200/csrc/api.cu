@@ -2311,9 +2311,15 @@ static prom_status run_forward(Fwd &p, bool wide, const DeviceInfo &d, cudaStrea
         if (whole <= 128 && !CODES) return launch_short<T, 4, false>(p, d, st);
         if (CODES ? p.n <= 4096 : whole <= 512) return launch_warps<T, CODES>(p, warps_for<T, CODES>(p, d), d, st);
     }
-    if (p.period && pieces <= 1024 && !wide) {
-        const int blocks = share_out(p, pieces, 1024, d);
-        return launch(forward_groups_kernel<T, CODES>, p, blocks, p.group * p.groups, 0, st);
+    if (p.period && pieces <= 2 * kGroupThreads && !wide) {
+        // (codes hold 64-bit sums beside the parameters: one piece a thread as long as they fit)
+        constexpr int V = CODES ? 1 : 2;
+        if (pieces <= V * kGroupThreads) {
+            const int blocks = share_out(p, (pieces + V - 1) / V, kGroupThreads, d);
+            return launch(forward_groups_kernel<T, V, CODES>, p, blocks, p.group * p.groups, 0, st);
+        }
+        const int blocks = share_out(p, (pieces + 1) / 2, kGroupThreads, d);
+        return launch(forward_groups_kernel<T, 2, CODES>, p, blocks, p.group * p.groups, 0, st);
     }
     if (wide) {
         if (p.n / E <= 2048) return launch_blocks<T, E, 2, CODES>(p, st);
@@ -2360,7 +2366,7 @@ static prom_status forward(const void *x, int type, int64_t m, int n, int64_t x_
 template <class T, int E, int V, bool RING>
 static prom_status launch_backward(Bwd &p, int pieces, const DeviceInfo &d, int &blocks, cudaStream_t st)
 {
-    blocks = share_out(p, (pieces + V - 1) / V, kBwdThreads<E, V>, d);
+    blocks = share_out(p, (pieces + V - 1) / V, kBwdThreads, d);
     p.stages = 0;
     size_t smem = p.part ? (size_t)2 * p.n_pad * 4 : 0;
     constexpr int kRoom = 10240;        // static shared memory and what the system keeps
@@ -2383,16 +2389,14 @@ static prom_status run_backward(Bwd &p, bool wide, const DeviceInfo &d, int &blo
     const int pieces = p.n / E, period = p.period;
     const int shifted = period ? (p.n + (period > 1 || !wide ? E - 1 : 0) + E - 1) / E : 0;
     // rows of less than a kilobyte come by plain loads too: a bulk copy each costs more than it moves
-    if (period && shifted <= (wide ? 64 : 1024)) return launch_backward<T, E, 1, false>(p, shifted, d, blocks, st);
+    if (period && shifted <= (wide ? 64 : 2 * kBwdThreads)) return launch_backward<T, E, 2, false>(p, shifted, d, blocks, st);
     p.period = 1;
     if (wide) {
-        if (pieces <= 1024) return launch_backward<T, E, 1, true>(p, pieces, d, blocks, st);
-        if (pieces <= 2 * kBwdThreads<E, 2>) return launch_backward<T, E, 2, true>(p, pieces, d, blocks, st);
-        if (pieces <= 4 * kBwdThreads<E, 4>) return launch_backward<T, E, 4, true>(p, pieces, d, blocks, st);
+        if (pieces <= 2 * kBwdThreads) return launch_backward<T, E, 2, true>(p, pieces, d, blocks, st);
+        if (pieces <= 4 * kBwdThreads) return launch_backward<T, E, 4, true>(p, pieces, d, blocks, st);
     } else {
-        if (p.n <= 1024) return launch_backward<T, 1, 1, false>(p, p.n, d, blocks, st);
-        if (p.n <= 4 * kBwdThreads<1, 4>) return launch_backward<T, 1, 4, false>(p, p.n, d, blocks, st);
-        if (p.n <= 16 * kBwdThreads<1, 16>) return launch_backward<T, 1, 16, false>(p, p.n, d, blocks, st);
+        if (p.n <= 4 * kBwdThreads) return launch_backward<T, 1, 4, false>(p, p.n, d, blocks, st);
+        if (p.n <= 16 * kBwdThreads) return launch_backward<T, 1, 16, false>(p, p.n, d, blocks, st);
     }
     // the column sums first: dx may be dy or x
     if (p.part) {
@@ -2987,7 +2991,7 @@ prom_status prom_layer_norm_backward(const void *dy_dev, const void *x_dev, prom
     else if (type == PROM_TYPE_BF16) s = norm::run_backward<__nv_bfloat16>(p, wide, d, blocks, st);
     else s = norm::run_backward<__half>(p, wide, d, blocks, st);
     if (s != PROM_OK || !sums) return s;
-    fill_launch_cfg(cfg, attr, (2 * p.n_pad + 127) / 128, 256, 0, st, true);
+    fill_launch_cfg(cfg, attr, (2 * p.n_pad + 127) / 128, 32 * norm::kSumWarps, 0, st, true);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, norm::backward_sum_kernel, (const float *)p.part, blocks, n, p.n_pad, dweight_dev,
                                              dbias_dev, pt);
     ++g_launches;

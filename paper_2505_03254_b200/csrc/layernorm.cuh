@@ -80,6 +80,11 @@ template <class T, int E> struct Piece {
     __device__ __forceinline__ Piece() : raw(make_uint4(0u, 0u, 0u, 0u)) {}
     __device__ __forceinline__ void load(const T *p) { raw = *reinterpret_cast<const uint4 *>(p); }
     __device__ __forceinline__ void store(T *p) const { *reinterpret_cast<uint4 *>(p) = raw; }
+    __device__ __forceinline__ void load_shared(uint32_t addr)
+    {
+        const int4 v = ptx::lds_128(addr);
+        raw = make_uint4((uint32_t)v.x, (uint32_t)v.y, (uint32_t)v.z, (uint32_t)v.w);
+    }
     __device__ __forceinline__ float get(int e) const
     {
         const int i = sizeof(T) == 4 ? e : e >> 1;
@@ -129,6 +134,7 @@ template <class T> struct Piece<T, 1> {
     __device__ __forceinline__ Piece() : v(from_float<T>(0.0f)) {}
     __device__ __forceinline__ void load(const T *p) { v = *p; }
     __device__ __forceinline__ void store(T *p) const { *p = v; }
+    __device__ __forceinline__ void load_shared(uint32_t) {}       // (rows in shared memory are whole pieces)
     __device__ __forceinline__ float get(int) const { return to_float<T>(v); }
     __device__ __forceinline__ void set(const float (&f)[1]) { v = from_float<T>(f[0]); }
     __device__ __forceinline__ void again() {}
@@ -391,9 +397,11 @@ __device__ __forceinline__ void parameters_of(const float *sw, const float *sb, 
 // Columns that the first piece of the row at `p` has before it.
 template <class T> __device__ __forceinline__ int offset_of(const void *p) { return (int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T)); }
 
-// ---- forward: groups ----------------------------------------------------------------------------------
-template <class T, bool CODES>
-__global__ void __launch_bounds__(1024, 1)
+// ---- forward: groups, for rows that start anywhere ------------------------------------------------------
+// V pieces a thread, two rows at a time and the next two on their way.
+constexpr int kGroupThreads = 512;
+template <class T, int V, bool CODES>
+__global__ void __launch_bounds__(kGroupThreads, 1)
 forward_groups_kernel(const Fwd p)
 {
     using Sum = typename std::conditional<CODES, double, float>::type;
@@ -407,66 +415,134 @@ forward_groups_kernel(const Fwd p)
     ptx::grid_dep_launch();
     if (r0 >= all || r0 >= m) return;           // (whole groups, which meet no other's threads)
     const T *x = static_cast<const T *>(p.x);
-    const int c = t * E - offset_of<T>(x + r0 * p.x_pitch);
-    const bool full = c >= 0 && c + E <= n, some = c + E > 0 && c < n;
-    float w[E], b[E];
-    p.w.get_at<E>(c, n, 1.0f, w);
-    p.b.get_at<E>(c, n, 0.0f, b);
+    const int c0 = t * E - offset_of<T>(x + r0 * p.x_pitch), hop = p.group * E;     // access i has columns c0 + i hop .. + E - 1
+    auto full = [&](int i) { return c0 + i * hop >= 0 && c0 + i * hop + E <= n; };
+    auto some = [&](int i) { return c0 + i * hop + E > 0 && c0 + i * hop < n; };
+    auto inside = [&](int i, int e) { return c0 + i * hop + e >= 0 && c0 + i * hop + e < n; };
+    float w[V][E], b[V][E];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        p.w.get_at<E>(c0 + i * hop, n, 1.0f, w[i]);
+        p.b.get_at<E>(c0 + i * hop, n, 0.0f, b[i]);
+    }
     const Sum inv_n = (Sum)1 / (Sum)n;
     // codes of a whole piece in one store
-    const bool wide_q = CODES && (reinterpret_cast<uintptr_t>(p.q) + (uint64_t)((long long)r0 * n + c)) % E == 0 && (long long)all * n % E == 0;
+    const bool wide_q = CODES && (reinterpret_cast<uintptr_t>(p.q) + (uint64_t)((long long)r0 * n + c0)) % E == 0 && (long long)all * n % E == 0;
 
-    Piece<T, E> v[2], next[2];
-    auto load = [&](int r, Piece<T, E> &to) {
-        to.raw = make_uint4(0u, 0u, 0u, 0u);
-        if (r < m && some) load_at<T, E>(to, x + (long long)r * p.x_pitch, c, n);
+    Piece<T, E> v[2][V], next[2][V];
+    auto load = [&](int r, Piece<T, E> (&to)[V]) {
+        const T *row = x + r * p.x_pitch;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            to[i].raw = make_uint4(0u, 0u, 0u, 0u);
+            if (r < m && some(i)) load_at<T, E>(to[i], row, c0 + i * hop, n);
+        }
     };
+    auto later = [&](int r, int k) { return (long long)r + (long long)k * all < m ? r + k * all : m; };
     load(r0, next[0]);
-    load(all < m - r0 ? r0 + all : m, next[1]);
+    load(later(r0, 1), next[1]);
 #pragma unroll 1
-    for (long long rr = r0; rr < m; rr += 2ll * all) {
-        const int r = (int)rr;
-        const bool two = (long long)r + all < m;
-        v[0] = next[0];
-        v[1] = next[1];
-        load(rr + 2ll * all < m ? (int)(rr + 2ll * all) : m, next[0]);
-        load(rr + 3ll * all < m ? (int)(rr + 3ll * all) : m, next[1]);
+    for (int r = r0; r < m; r = later(r, 2)) {
+        const bool two = later(r, 1) < m;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[k][i] = next[k][i];
+        load(later(r, 2), next[0]);
+        load(later(r, 3), next[1]);
         Sum s[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             s[k] = 0;
-            if constexpr (CODES) {
-                float odd = 0.0f;               // NaN once a value is not finite
+#pragma unroll
+            for (int i = 0; i < V; ++i)
 #pragma unroll
                 for (int e = 0; e < E; ++e) {   // (what lies outside the row is zero)
-                    const float f = v[k].get(e);
-                    s[k] = fma(scaled_down<T>(f), two_896(), s[k]);
-                    odd = fmaf(f, 0.0f, odd);
+                    if constexpr (CODES) s[k] = fma(scaled_down<T>(v[k][i].get(e)), two_896(), s[k]);
+                    else s[k] += v[k][i].get(e);
                 }
-                s[k] += (double)odd;
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) s[k] += v[k].get(e);
-            }
         }
         Sum mean[2];
         spread_2(group_sum_2(s[0], s[1], red_mean, g, p.group) * inv_n, mean);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             s[k] = 0;
-            v[k].again();
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                Sum d;
-                if constexpr (CODES) d = fma(scaled_down<T>(v[k].get(e)), two_896(), -mean[k]);
-                else d = v[k].get(e) - mean[k];
-                if (full || (c + e >= 0 && c + e < n)) s[k] = fma(d, d, s[k]);
+            for (int i = 0; i < V; ++i) {
+                v[k][i].again();
+                if (some(i)) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        Sum d;
+                        if constexpr (CODES) d = fma(scaled_down<T>(v[k][i].get(e)), two_896(), -mean[k]);
+                        else d = v[k][i].get(e) - mean[k];
+                        if (full(i) || inside(i, e)) s[k] = fma(d, d, s[k]);
+                    }
+                }
             }
         }
         const float rstd_half = (float)inverse_root(group_sum_2(s[0], s[1], red_var, g, p.group) * inv_n + (Sum)p.eps);
-        const float mu[2] = {(float)mean[0], (float)mean[1]};
-        float rstd[2];
+        float mu[2] = {(float)mean[0], (float)mean[1]}, rstd[2];
         spread_2(rstd_half, rstd);
+        if constexpr (!CODES) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if (k && !two) continue;
+                T *row = static_cast<T *>(p.y) + (r + k * all) * p.y_pitch;
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (some(i)) {
+                        v[k][i].again();
+                        float f[E];
+#pragma unroll
+                        for (int e = 0; e < E; ++e) f[e] = (v[k][i].get(e) - mu[k]) * rstd[k] * w[i][e] + b[i][e];
+                        Piece<T, E> o;
+                        o.set(f);
+                        store_at<T, E>(o, row, c0 + i * hop, n);
+                    }
+            }
+        } else {
+            float top[2], scale[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                top[k] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (some(i)) {
+                        v[k][i].again();
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            if (full(i) || inside(i, e))
+                                top[k] = max_nan(top[k], fabsf(affine_exact(v[k][i].get(e), mu[k], rstd[k], w[i][e], b[i][e])));
+                    }
+            }
+            const float top_half = group_max_2(top[0], top[1], red_max, g, p.group);
+            spread_2(top_half, top);
+            spread_2(actq::scale_of(top_half, 1e-5f), scale);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if (k && !two) continue;
+                if (t == 0) { p.gamma[r + k * all] = top[k]; p.scale[r + k * all] = scale[k]; }
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (some(i)) {
+                        v[k][i].again();        // computed again: kept, the values would take more registers than there are
+                        float f[E];
+#pragma unroll
+                        for (int e = 0; e < E; ++e) f[e] = affine_exact(v[k][i].get(e), mu[k], rstd[k], w[i][e], b[i][e]);
+                        int8_t *out = p.q + (long long)(r + k * all) * n + c0 + i * hop;
+                        if (full(i) && wide_q) {
+                            store_codes<E>(out, f, scale[k]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < E; ++e)
+                                if (inside(i, e)) out[e] = actq::quantise_one(f[e], scale[k]);
+                        }
+                    }
+                // (a value that is not finite shows in the maximum only: the sums took its bits for a number's)
+                if (!(top[k] <= 3.402823466e38f)) mu[k] = rstd[k] = __int_as_float(0x7FC00000);
+            }
+        }
         if (t == 0) {
 #pragma unroll
             for (int k = 0; k < 2; ++k)
@@ -474,52 +550,6 @@ forward_groups_kernel(const Fwd p)
                     if (p.mean) p.mean[r + k * all] = mu[k];
                     if (p.rstd) p.rstd[r + k * all] = rstd[k];
                 }
-        }
-        if constexpr (!CODES) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                if ((k && !two) || !some) continue;
-                v[k].again();
-                float f[E];
-#pragma unroll
-                for (int e = 0; e < E; ++e) f[e] = (v[k].get(e) - mu[k]) * rstd[k] * w[e] + b[e];
-                Piece<T, E> o;
-                o.set(f);
-                store_at<T, E>(o, static_cast<T *>(p.y) + (long long)(r + k * all) * p.y_pitch, c, n);
-            }
-        } else {
-            float top[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                top[k] = 0.0f;
-                v[k].again();
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (full || (c + e >= 0 && c + e < n)) top[k] = max_nan(top[k], fabsf(affine_exact(v[k].get(e), mu[k], rstd[k], w[e], b[e])));
-            }
-            const float top_half = group_max_2(top[0], top[1], red_max, g, p.group);
-            float scale[2];
-            spread_2(top_half, top);
-            spread_2(actq::scale_of(top_half, 1e-5f), scale);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                if (k && !two) continue;
-                const float sc = scale[k];
-                if (t == 0) { p.gamma[r + k * all] = top[k]; p.scale[r + k * all] = sc; }
-                if (!some) continue;
-                v[k].again();                   // computed again: kept, the values would take more registers than there are
-                float f[E];
-#pragma unroll
-                for (int e = 0; e < E; ++e) f[e] = affine_exact(v[k].get(e), mu[k], rstd[k], w[e], b[e]);
-                int8_t *out = p.q + (long long)(r + k * all) * n + c;
-                if (full && wide_q) {
-                    store_codes<E>(out, f, sc);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (c + e >= 0 && c + e < n) out[e] = actq::quantise_one(f[e], sc);
-                }
-            }
         }
     }
 }
@@ -929,35 +959,37 @@ struct Bwd {
 
 constexpr int kMaxGroups = 32;
 constexpr int kMaxStages = 16;              // rows of a group's ring
-// One piece a thread (up to 1024 to a row): as many threads as an SM has; two rows at a time out of the ring, one with the next
-// one on its way without it.  More: fewer threads, for their column sums are registers (2 V E of them).
-template <int E, int V> constexpr int kBwdThreads = V * E >= 32 || V >= 16 ? 512 : (V * E > 8 ? 768 : 1024);
-template <int V, bool RING> constexpr int kBwdRows = V == 1 && RING ? 2 : 1;
+// Two pieces a thread, and two rows at a time out of the ring (one, with the next one on its way, without it): what a row costs
+// beside its values, the exchange and the addresses, is then spread over 16 or 32 of them, and the column sums (2 V E),
+// weights and rows still fit the registers.  More pieces: one row at a time.
+constexpr int kBwdThreads = 512;             // (768 with fewer registers: 25088 x 960 float32 72 us instead of 52)
+template <int V, bool RING> constexpr int kBwdRows = V <= 2 && RING ? 2 : 1;
 
 // RING: rows come through shared memory by bulk copies (whole 16-byte pieces), else by plain loads.
 // Shared memory: the rings ([groups][stages][2][row bytes]), used again at the end for the groups' column sums.
 template <class T, int E, int V, bool RING>
-__global__ void __launch_bounds__(kBwdThreads<E, V>, 1)
+__global__ void __launch_bounds__(kBwdThreads, 1)
 backward_kernel(const Bwd p)
 {
     constexpr int R = kBwdRows<V, RING>;
-    constexpr bool kShift = !RING && V == 1 && E > 1;       // rows may start anywhere
+    constexpr bool kShift = !RING && E > 1;     // rows may start anywhere
+    constexpr bool kHoldW = V * E <= 16;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t bars[RING ? kMaxGroups * kMaxStages : 1];
     __shared__ float4 red[2][32];
     __shared__ volatile int failed;
     const int g = (int)threadIdx.x / p.group, t = (int)threadIdx.x - g * p.group;
     const int lane = threadIdx.x & 31, warps = p.group >> 5, first_warp = g * warps;
-    const int n = p.n, pieces = n / E;
+    const int n = p.n, m = (int)p.m;
     const uint32_t row_bytes = (uint32_t)n * (uint32_t)sizeof(T);
-    const uint32_t ring = ptx::smem_u32(smem) + (uint32_t)g * p.stages * 2u * row_bytes;
+    const uint32_t ring = ptx::smem_u32(smem) + (uint32_t)(g * p.stages) * 2u * row_bytes + (uint32_t)t * 16u;
     const uint32_t bar0 = ptx::smem_u32(bars) + 8u * (uint32_t)(g * p.stages);
-    const long long step = (long long)((int)gridDim.x * p.groups / p.period * p.period);
-    const long long first = (long long)g * gridDim.x + blockIdx.x, r0 = first < step ? first : p.m;     // (the last rows go round the SMs)
+    const int step = (int)gridDim.x * p.groups / p.period * p.period;
+    const int r0 = g * (int)gridDim.x + (int)blockIdx.x < step ? g * (int)gridDim.x + (int)blockIdx.x : m;      // (the last rows go round the SMs)
     const T *x = static_cast<const T *>(p.x), *dy = static_cast<const T *>(p.dy);
-    const int c0 = kShift ? t * E - (r0 < p.m ? offset_of<T>(x + r0 * p.x_pitch) : 0) : 0;
-    // whether access i of this thread is in the row
-    auto in_row = [&](int i) { return kShift ? c0 + E > 0 && c0 < n : t + i * p.group < pieces; };
+    const int c0 = t * E - (kShift && r0 < m ? offset_of<T>(x + r0 * p.x_pitch) : 0), hop = p.group * E;
+    // access i has columns c0 + i hop .. + E - 1
+    auto in_row = [&](int i) { return kShift ? c0 + i * hop + E > 0 && c0 + i * hop < n : c0 + i * hop < n; };
 
     if (RING) {
         if (t < p.stages) ptx::mbar_init(bar0 + 8u * t, 1);
@@ -967,90 +999,86 @@ backward_kernel(const Bwd p)
     __syncthreads();
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
-    auto fetch = [&](int s, long long r) {      // by one thread of the group
+    auto fetch = [&](uint32_t s, long long r) {      // by one thread of the group (t == 0)
         ptx::mbar_expect_tx(bar0 + 8u * s, 2u * row_bytes);
-        ptx::bulk_load(ring + (uint32_t)s * 2u * row_bytes, x + r * p.x_pitch, row_bytes, bar0 + 8u * s);
-        ptx::bulk_load(ring + (uint32_t)s * 2u * row_bytes + row_bytes, dy + r * p.dy_pitch, row_bytes, bar0 + 8u * s);
+        ptx::bulk_load(ring + s * 2u * row_bytes, x + r * p.x_pitch, row_bytes, bar0 + 8u * s);
+        ptx::bulk_load(ring + s * 2u * row_bytes + row_bytes, dy + r * p.dy_pitch, row_bytes, bar0 + 8u * s);
     };
     long long ahead = r0;                       // the next row to fetch (kept by that thread)
     if (RING && t == 0)
-        for (int s = 0; s < p.stages && ahead < p.m; ++s, ahead += step) fetch(s, ahead);
+        for (int s = 0; s < p.stages && ahead < m; ++s, ahead += step) fetch((uint32_t)s, ahead);
 
-    constexpr bool kHoldW = V * E < 16;
     float held[kHoldW ? V : 1][E], dw[V][E], db[V][E];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        if constexpr (kShift) p.w.get_at<E>(c0, n, 1.0f, held[0]);
-        else if constexpr (kHoldW)
-            if (t + i * p.group < pieces) p.w.get<E>((t + i * p.group) * E, 1.0f, held[i]);
+        if constexpr (kHoldW) p.w.get_at<E>(c0 + i * hop, n, 1.0f, held[i]);
 #pragma unroll
         for (int e = 0; e < E; ++e) dw[i][e] = db[i][e] = 0.0f;
     }
-    const float inv_n = 1.0f / (float)p.n;
-    int s = 0, which = 0;
-    uint32_t phase = 0;
+    const float inv_n = 1.0f / (float)n;
     float next_mean[R], next_rstd[R];           // of the rows behind the current ones: not waited for
-    auto statistics = [&](long long r) {
+    auto statistics = [&](int r) {
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            const long long rk = r + k * step;
-            next_mean[k] = rk < p.m ? __ldg(p.mean + rk) : 0.0f;
-            next_rstd[k] = rk < p.m ? __ldg(p.rstd + rk) : 0.0f;
+            const bool there = k == 0 ? r < m : step < m - r;
+            next_mean[k] = there ? __ldg(p.mean + r + k * step) : 0.0f;
+            next_rstd[k] = there ? __ldg(p.rstd + r + k * step) : 0.0f;
         }
     };
     statistics(r0);
     Piece<T, E> next_x[RING ? 1 : V], next_d[RING ? 1 : V];
-    auto load = [&](long long r) {
+    auto load = [&](int r) {
 #pragma unroll
         for (int i = 0; i < (RING ? 1 : V); ++i)
-            if (r < p.m && in_row(i)) {
+            if (r < m && in_row(i)) {
                 const T *xr = x + r * p.x_pitch, *dr = dy + r * p.dy_pitch;
                 if constexpr (kShift) {
-                    load_at<T, E>(next_x[i], xr, c0, n);
-                    load_at<T, E>(next_d[i], dr, c0, n);
+                    load_at<T, E>(next_x[i], xr, c0 + i * hop, n);
+                    load_at<T, E>(next_d[i], dr, c0 + i * hop, n);
                 } else {
-                    next_x[i].load(xr + (size_t)(t + i * p.group) * E);
-                    next_d[i].load(dr + (size_t)(t + i * p.group) * E);
+                    next_x[i].load(xr + c0 + i * hop);
+                    next_d[i].load(dr + c0 + i * hop);
                 }
             }
     };
     if constexpr (!RING) load(r0);
+    uint32_t s = 0, phase = 0;                  // the ring's stage of the first row
+    int which = 0;
+    T *out = static_cast<T *>(p.dx) + (r0 < m ? r0 * p.dx_pitch : 0) + c0;
+    const long long out_step = (long long)step * p.dx_pitch;
 #pragma unroll 1
-    for (long long r = r0; r < p.m; r += R * step) {
+    for (int r = r0; r < m;) {
+        const bool two = R == 2 && step < m - r;
+        const int after = (R == 2 ? two && step < m - r - step : step < m - r) ? r + R * step : m;
         float mean[R], rstd[R], s1[R], s2[R];   // sums of g and of g xh
         Piece<T, E> vx[R][V], vd[R][V];
 #pragma unroll
         for (int k = 0; k < R; ++k) { mean[k] = next_mean[k]; rstd[k] = next_rstd[k]; }
-        statistics(r + R * step);
+        statistics(after);
+        if constexpr (RING) {
 #pragma unroll
-        for (int k = 0; k < R; ++k) {
-            const long long rk = r + k * step;
-            const bool there = rk < p.m;
-            if constexpr (RING) {
-                if (there) {
+            for (int k = 0; k < R; ++k)
+                if (k == 0 || two) {
                     // A wait that runs out is the last one: the block goes on without waiting, so that its barriers stay in
                     // step, fetches nothing more and reports at the end.
-                    const int st = s + k < p.stages ? s + k : s + k - p.stages;
-                    const uint32_t ph = s + k < p.stages ? phase : phase ^ 1u;
+                    const uint32_t st = s + k < (uint32_t)p.stages ? s + k : 0u, ph = s + k < (uint32_t)p.stages ? phase : phase ^ 1u;
                     if (!ptx::mbar_try_wait(bar0 + 8u * st, ph)) {
                         const unsigned long long t0 = ptx::globaltimer();
                         while (!ptx::mbar_try_wait(bar0 + 8u * st, ph))
                             if (failed || ptx::globaltimer() - t0 > actq::kWaitLimitNs) { failed = 1; break; }
                     }
-                    const T *sx = reinterpret_cast<const T *>(smem + (size_t)(g * p.stages + st) * 2 * row_bytes);
-                    const T *sd = reinterpret_cast<const T *>(smem + (size_t)(g * p.stages + st) * 2 * row_bytes + row_bytes);
+                    const uint32_t at = ring + st * 2u * row_bytes;
 #pragma unroll
                     for (int i = 0; i < V; ++i)
-                        if (t + i * p.group < pieces) {
-                            vx[k][i].load(sx + (size_t)(t + i * p.group) * E);
-                            vd[k][i].load(sd + (size_t)(t + i * p.group) * E);
+                        if (in_row(i)) {
+                            vx[k][i].load_shared(at + (uint32_t)(i * p.group) * 16u);
+                            vd[k][i].load_shared(at + row_bytes + (uint32_t)(i * p.group) * 16u);
                         }
                 }
-            } else {
+        } else {
 #pragma unroll
-                for (int i = 0; i < V; ++i) { vx[k][i] = next_x[RING ? 0 : i]; vd[k][i] = next_d[RING ? 0 : i]; }
-                load(r + step);
-            }
+            for (int i = 0; i < V; ++i) { vx[0][i] = next_x[RING ? 0 : i]; vd[0][i] = next_d[RING ? 0 : i]; }
+            load(after);
         }
 #pragma unroll
         for (int k = 0; k < R; ++k) {
@@ -1059,7 +1087,7 @@ backward_kernel(const Bwd p)
             for (int i = 0; i < V; ++i)
                 if (in_row(i)) {
                     float w[E];
-                    if constexpr (!kHoldW) p.w.get<E>((t + i * p.group) * E, 1.0f, w);
+                    if constexpr (!kHoldW) p.w.get_at<E>(c0 + i * hop, n, 1.0f, w);
 #pragma unroll
                     for (int e = 0; e < E; ++e) {       // (a row that is not there is one of zeros, as is dy outside a row)
                         const float we = kHoldW ? held[kHoldW ? i : 0][e] : w[e];
@@ -1071,55 +1099,59 @@ backward_kernel(const Bwd p)
                     }
                 }
         }
-        float v = R == 2 ? warp_sum_4(s1[0], s2[0], s1[R - 1], s2[R - 1]) : warp_sum_4(s1[0], s2[0], 0.0f, 0.0f);
+        float v = R == 2 ? warp_sum_4(s1[0], s2[0], s1[R - 1], s2[R - 1]) : warp_sum_2(s1[0], s2[0]);
+        constexpr int kValues = 2 * R, kSpan = 32 / kValues;
         if (warps > 1) {
-            if ((lane & 7) == 0) reinterpret_cast<float *>(&red[which][threadIdx.x >> 5])[lane >> 3] = v;
+            if ((lane & (kSpan - 1)) == 0) reinterpret_cast<float *>(&red[which][threadIdx.x >> 5])[lane / kSpan] = v;
             group_barrier(g, p.group);
             // every thread of the group has read its part of the stages, so they can be filled again
             const float4 a = lane < warps ? red[which][first_warp + lane] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            v = warp_sum_4(a.x, a.y, a.z, a.w);
+            v = R == 2 ? warp_sum_4(a.x, a.y, a.z, a.w) : warp_sum_2(a.x, a.y);
             which ^= 1;                         // the next rows' sums go elsewhere: these may still be read
         } else {
             __syncwarp();
         }
-        float unused1, unused2;
-        if constexpr (R == 2) spread_4(v, s1[0], s2[0], s1[R - 1], s2[R - 1]);
-        else spread_4(v, s1[0], s2[0], unused1, unused2);
+        v *= inv_n;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            s1[k] = __shfl_sync(0xFFFFFFFFu, v, 2 * k * kSpan);
+            s2[k] = __shfl_sync(0xFFFFFFFFu, v, (2 * k + 1) * kSpan);
+        }
         if (RING) {
             if (t == 0 && !failed) {
 #pragma unroll
                 for (int k = 0; k < R; ++k)
-                    if (ahead < p.m) { fetch(s + k < p.stages ? s + k : s + k - p.stages, ahead); ahead += step; }
+                    if (ahead < m) { fetch(s + k < (uint32_t)p.stages ? s + k : 0u, ahead); ahead += step; }
             }
             s += R;
-            if (s >= p.stages) { s -= p.stages; phase ^= 1u; }
+            if (s >= (uint32_t)p.stages) { s -= (uint32_t)p.stages; phase ^= 1u; }
         }
         if (p.dx) {
 #pragma unroll
-            for (int k = 0; k < R; ++k) {
-                const long long rk = r + k * step;
-                const float c1 = s1[k] * inv_n, c2 = s2[k] * inv_n;
-                T *out = static_cast<T *>(p.dx) + rk * p.dx_pitch;
+            for (int k = 0; k < R; ++k)
+                if (k == 0 || two) {
 #pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (rk < p.m && in_row(i)) {
-                        float w[E];
-                        if constexpr (!kHoldW) p.w.get<E>((t + i * p.group) * E, 1.0f, w);
-                        vx[k][i].again();
-                        vd[k][i].again();
+                    for (int i = 0; i < V; ++i)
+                        if (in_row(i)) {
+                            float w[E];
+                            if constexpr (!kHoldW) p.w.get_at<E>(c0 + i * hop, n, 1.0f, w);
+                            vx[k][i].again();
+                            vd[k][i].again();
 #pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            const float we = kHoldW ? held[kHoldW ? i : 0][e] : w[e];
-                            const float xh = (vx[k][i].get(e) - mean[k]) * rstd[k];
-                            w[e] = rstd[k] * (vd[k][i].get(e) * we - c1 - xh * c2);
+                            for (int e = 0; e < E; ++e) {
+                                const float we = kHoldW ? held[kHoldW ? i : 0][e] : w[e];
+                                const float xh = (vx[k][i].get(e) - mean[k]) * rstd[k];
+                                w[e] = rstd[k] * (vd[k][i].get(e) * we - s1[k] - xh * s2[k]);
+                            }
+                            Piece<T, E> o;
+                            o.set(w);
+                            if constexpr (kShift) store_at<T, E>(o, out + k * out_step - c0, c0 + i * hop, n);
+                            else o.store(out + k * out_step + i * hop);
                         }
-                        Piece<T, E> o;
-                        o.set(w);
-                        if constexpr (kShift) store_at<T, E>(o, out, c0, n);
-                        else o.store(out + (size_t)(t + i * p.group) * E);
-                    }
-            }
+                }
+            out += R * out_step;
         }
+        r = after;
     }
     __syncthreads();
     if (RING && failed) {
@@ -1140,7 +1172,7 @@ backward_kernel(const Bwd p)
 #pragma unroll
             for (int i = 0; i < V; ++i)
                 if (in_row(i)) {
-                    const int c = kShift ? c0 : (t + i * p.group) * E;
+                    const int c = c0 + i * hop;
 #pragma unroll
                     for (int e = 0; e < E; ++e)
                         if (!kShift || (c + e >= 0 && c + e < n)) {
@@ -1201,19 +1233,20 @@ column_sums_kernel(const Bwd p, long long rows_per_block)
     mine[p.n_pad + c] = db;
 }
 
-// The sums over the blocks' partial sums: eight warps share 128 columns, each every eighth block, then one adds the eight.
-__global__ void __launch_bounds__(256)
+// The sums over the blocks' partial sums: 32 warps share 128 columns, each every 32nd block, then one adds the 32.
+constexpr int kSumWarps = 32;
+__global__ void __launch_bounds__(32 * kSumWarps)
 backward_sum_kernel(const float *__restrict__ part, int blocks, int n, int n_pad, void *dw, void *db, int type)
 {
-    __shared__ float4 s[8][32];
+    __shared__ float4 s[kSumWarps][32];
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int c = blockIdx.x * 128 + lane * 4;          // of the 2 n_pad columns
     float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (c < 2 * n_pad) {
-#pragma unroll 4
-        for (int k = warp; k < blocks; k += 8) {
+#pragma unroll 8
+        for (int k = warp; k < blocks; k += kSumWarps) {
             const float4 v = *reinterpret_cast<const float4 *>(part + (size_t)k * 2 * n_pad + c);
             a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
         }
@@ -1222,7 +1255,7 @@ backward_sum_kernel(const float *__restrict__ part, int blocks, int n, int n_pad
     __syncthreads();
     if (warp || c >= 2 * n_pad) return;
 #pragma unroll
-    for (int k = 1; k < 8; ++k) { const float4 v = s[k][lane]; a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w; }
+    for (int k = 1; k < kSumWarps; ++k) { const float4 v = s[k][lane]; a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w; }
     void *out = c < n_pad ? dw : db;
     if (!out) return;
     const int c0 = c < n_pad ? c : c - n_pad;

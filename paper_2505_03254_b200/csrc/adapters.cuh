@@ -105,25 +105,40 @@ template <class H> __device__ __forceinline__ float finite(float v, bool &bad)
     bad |= !ok;
     return ok ? v : 0.0f;
 }
+// The first sixteen values of a row of B, which can be on their way before the inner products are there.
+struct Ahead {
+    uint4 v[2];
+    template <class H> __device__ __forceinline__ void load(const Params &p, int a, int o)
+    {
+        if (p.rank & 7) return;
+        const uint4 *b = reinterpret_cast<const uint4 *>(static_cast<const H *>(p.b) + ((size_t)a * p.cout + o) * p.rank);
+        v[0] = __ldg(b);
+        if (p.rank > 8) v[1] = __ldg(b + 1);
+    }
+};
+template <class H> __device__ __forceinline__ float outer_8(const uint4 &v, const float *t, float s, bool &bad)
+{
+    const float4 t0 = *reinterpret_cast<const float4 *>(t), t1 = *reinterpret_cast<const float4 *>(t + 4);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    const float tt[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = unpack_2<H>(w[i]);
+        s = fmaf(finite<H>(f.x, bad), tt[2 * i], s);
+        s = fmaf(finite<H>(f.y, bad), tt[2 * i + 1], s);
+    }
+    return s;
+}
 template <class H>
-__device__ __forceinline__ float outer(const Params &p, int a, int o, const float *t, bool &bad)
+__device__ __forceinline__ float outer(const Params &p, int a, int o, const float *t, const Ahead &ahead, bool &bad)
 {
     const H *b = static_cast<const H *>(p.b) + ((size_t)a * p.cout + o) * p.rank;
     float s = 0.0f;
     if ((p.rank & 7) == 0) {
+        s = outer_8<H>(ahead.v[0], t, s, bad);
+        if (p.rank > 8) s = outer_8<H>(ahead.v[1], t + 8, s, bad);
 #pragma unroll 4
-        for (int j = 0; j < p.rank; j += 8) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4 *>(b + j));
-            const float4 t0 = *reinterpret_cast<const float4 *>(t + j), t1 = *reinterpret_cast<const float4 *>(t + j + 4);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-            const float tt[8] = {t0.x, t0.y, t0.z, t0.w, t1.x, t1.y, t1.z, t1.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = unpack_2<H>(w[i]);
-                s = fmaf(finite<H>(f.x, bad), tt[2 * i], s);
-                s = fmaf(finite<H>(f.y, bad), tt[2 * i + 1], s);
-            }
-        }
+        for (int j = 16; j < p.rank; j += 8) s = outer_8<H>(__ldg(reinterpret_cast<const uint4 *>(b + j)), t + j, s, bad);
     } else {
         for (int j = 0; j < p.rank; ++j) s = fmaf(finite<H>(norm::to_float(b[j]), bad), t[j], s);
     }
@@ -271,6 +286,7 @@ proj_rows_kernel(const Params p)
     constexpr int kEach = (128 * MO * MT + 32 * WARPS - 1) / (32 * WARPS);      // outputs of a thread
     float y[kEach], f[kEach];
     int a[kEach];
+    Ahead ahead[kEach];
 #pragma unroll
     for (int q = 0; q < kEach; ++q) {
         const int i = threadIdx.x + q * 32 * WARPS, o = i % (16 * MO), c = i / (16 * MO);
@@ -287,7 +303,10 @@ proj_rows_kernel(const Params p)
         f[q] = row_factor(p, s);
         y[q] = (float)(acc - 2 * sum) * __ldg(p.alpha + o0 + o) * f[q];
         a[q] = adapter_of(p, s);
-        if (a[q] >= 0 && p.scale) f[q] *= __ldg(p.scale + a[q]);
+        if (a[q] >= 0) {
+            if (p.scale) f[q] *= __ldg(p.scale + a[q]);
+            ahead[q].template load<H>(p, a[q], o0 + o);
+        }
     }
     if (p.chained) ptx::grid_dep_wait();        // for the inner products
     bool bad = false;
@@ -296,7 +315,7 @@ proj_rows_kernel(const Params p)
         const int i = threadIdx.x + q * 32 * WARPS, o = i % (16 * MO), c = i / (16 * MO);
         const long long r = r0 + c;
         if (c >= 8 * MT || r >= p.m || o0 + o >= p.cout) continue;
-        if (a[q] >= 0) y[q] += f[q] * outer<H>(p, a[q], o0 + o, p.t + r * p.rank, bad);
+        if (a[q] >= 0) y[q] += f[q] * outer<H>(p, a[q], o0 + o, p.t + r * p.rank, ahead[q], bad);
         static_cast<Y *>(p.y)[r * p.y_pitch + o0 + o] = norm::from_float<Y>(y[q]);
     }
     if (bad) raise_status(PROM_ERR_BAD_WEIGHT);

@@ -2588,9 +2588,10 @@ static prom_status run_tiles(Params &p, int y_type, const DeviceInfo &d, cudaStr
         p.power = reinterpret_cast<float *>(ws + t16_bytes(p.m, p.rank));
         p.row_adapter = reinterpret_cast<int *>(ws + t16_bytes(p.m, p.rank) + round256((size_t)p.m * sizeof(float)));
         p.list = reinterpret_cast<int *>(ws + t16_bytes(p.m, p.rank) + 2 * round256((size_t)p.m * sizeof(float)));
-        // a tile's items over several blocks: eight of a run of 256 rows, more where there are few tiles
-        long long share = (2ll * d.sms + q.n_mtiles - 1) / q.n_mtiles;
-        share = share < 8 ? 8 : (share > 32 ? 32 : share);
+        // A tile's items (eight of a run of 256 rows, more of many adapters) over several blocks, as many as the device holds at
+        // once: each sorts the tile first, which takes as long as one or two items.
+        long long share = 2ll * d.sms / q.n_mtiles;
+        share = share < 1 ? 1 : (share > 32 ? 32 : share);
         const dim3 grid((unsigned)q.n_mtiles, (unsigned)share);
         const cudaError_t e = p.pitch <= 16   ? launch_inner<H, 16>(p, grid, st)
                               : p.pitch <= 32 ? launch_inner<H, 32>(p, grid, st)

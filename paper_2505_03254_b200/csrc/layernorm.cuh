@@ -398,8 +398,9 @@ __device__ __forceinline__ void parameters_of(const float *sw, const float *sb, 
 template <class T> __device__ __forceinline__ int offset_of(const void *p) { return (int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T)); }
 
 // ---- forward: groups, for rows that start anywhere ------------------------------------------------------
-// V pieces a thread, two rows at a time and the next two on their way.
-constexpr int kGroupThreads = 512;
+// V pieces a thread, two rows at a time and the next two on their way.  (576 threads are two groups for rows of 4096 and
+// some values: 8192 x 4269 bf16 70 us, 100 with 512.)
+constexpr int kGroupThreads = 576;
 template <class T, int V, bool CODES>
 __global__ void __launch_bounds__(kGroupThreads, 1)
 forward_groups_kernel(const Fwd p)
@@ -688,14 +689,18 @@ forward_warps_kernel(const Fwd p)
         if (__any_sync(0xFFFFFFFFu, failed)) break;
         Piece<T, E> v;
         Sum s = 0, s2 = 0;
+        [[maybe_unused]] Sum sq = 0, sq2 = 0;
 #pragma unroll 4
         for (int i = lane; i < pieces; i += 32) {
             v.raw = mine[i];
 #pragma unroll
             for (int e = 0; e < E; e += 2) {
                 if constexpr (CODES) {
-                    s = fma(scaled_down<T>(v.get(e)), two_896(), s);
-                    s2 = fma(scaled_down<T>(v.get(e + 1)), two_896(), s2);
+                    const double d = scaled_down<T>(v.get(e)) * two_896(), d2 = scaled_down<T>(v.get(e + 1)) * two_896();
+                    s += d;
+                    s2 += d2;
+                    sq = fma(d, d, sq);
+                    sq2 = fma(d2, d2, sq2);
                 } else {
                     s += v.get(e);
                     s2 += v.get(e + 1);
@@ -703,25 +708,36 @@ forward_warps_kernel(const Fwd p)
             }
         }
         const Sum mean = warp_sum(s + s2) * inv_n;
-        s = s2 = 0;
-#pragma unroll 4
-        for (int i = lane; i < pieces; i += 32) {
-            v.raw = mine[i];
-#pragma unroll
-            for (int e = 0; e < E; e += 2) {
-                Sum d, d2;
-                if constexpr (CODES) {
-                    d = fma(scaled_down<T>(v.get(e)), two_896(), -mean);
-                    d2 = fma(scaled_down<T>(v.get(e + 1)), two_896(), -mean);
-                } else {
-                    d = v.get(e) - mean;
-                    d2 = v.get(e + 1) - mean;
-                }
-                s = fma(d, d, s);
-                s2 = fma(d2, d2, s2);
-            }
+        // In 64 bits the squares of the values (exact there) can be summed on the same pass: what their difference to the mean's
+        // square loses is seen, and where it is more than twelve bits the differences are taken after all.
+        Sum var = 0;
+        bool again = true;
+        if constexpr (CODES) {
+            var = fma(-mean, mean, warp_sum(sq + sq2) * inv_n);
+            again = !(var * 4096.0 >= mean * mean);
         }
-        float mu = (float)mean, rstd = (float)inverse_root(warp_sum(s + s2) * inv_n + (Sum)p.eps);
+        if (again) {
+            s = s2 = 0;
+#pragma unroll 4
+            for (int i = lane; i < pieces; i += 32) {
+                v.raw = mine[i];
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    Sum d, d2;
+                    if constexpr (CODES) {
+                        d = fma(scaled_down<T>(v.get(e)), two_896(), -mean);
+                        d2 = fma(scaled_down<T>(v.get(e + 1)), two_896(), -mean);
+                    } else {
+                        d = v.get(e) - mean;
+                        d2 = v.get(e + 1) - mean;
+                    }
+                    s = fma(d, d, s);
+                    s2 = fma(d2, d2, s2);
+                }
+            }
+            var = warp_sum(s + s2) * inv_n;
+        }
+        float mu = (float)mean, rstd = (float)inverse_root(var + (Sum)p.eps);
         if constexpr (!CODES) {
             T *out = static_cast<T *>(p.y) + r * p.y_pitch;
 #pragma unroll 2

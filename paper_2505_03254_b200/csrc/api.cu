@@ -2368,7 +2368,7 @@ static prom_status launch_backward(Bwd &p, int pieces, const DeviceInfo &d, int 
 {
     blocks = share_out(p, (pieces + V - 1) / V, kBwdThreads, d);
     p.stages = 0;
-    size_t smem = p.part ? (size_t)2 * p.n_pad * 4 : 0;
+    size_t smem = p.part ? (size_t)p.groups * 2 * p.n_pad * 4 : 0;
     constexpr int kRoom = 10240;        // static shared memory and what the system keeps
     if (RING) {
         // rows in flight: as many as fit, but a whole number of steps

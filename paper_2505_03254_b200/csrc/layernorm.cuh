@@ -1179,28 +1179,28 @@ backward_kernel(const Bwd p)
     }
     if (!p.part) return;
 
-    // The groups' column sums, added in the order of the groups; all copies have landed and been read.
-    float *acc = reinterpret_cast<float *>(smem);       // [2][n_pad]
-    for (int c = threadIdx.x; c < 2 * p.n_pad; c += blockDim.x) acc[c] = 0.0f;
-    __syncthreads();
-    for (int k = 0; k < p.groups; ++k) {
-        if (g == k) {
+    // The groups' column sums side by side ([groups][2][n_pad]), then added in the order of the groups; all copies have landed
+    // and been read.
+    float *acc = reinterpret_cast<float *>(smem), *own = acc + (size_t)g * 2 * p.n_pad;
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (in_row(i)) {
-                    const int c = c0 + i * hop;
+    for (int i = 0; i < V; ++i)
+        if (g < p.groups && in_row(i)) {
+            const int c = c0 + i * hop;
 #pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (!kShift || (c + e >= 0 && c + e < n)) {
-                            acc[c + e] += dw[i][e];
-                            acc[p.n_pad + c + e] += db[i][e];
-                        }
+            for (int e = 0; e < E; ++e)
+                if (!kShift || (c + e >= 0 && c + e < n)) {
+                    own[c + e] = dw[i][e];
+                    own[p.n_pad + c + e] = db[i][e];
                 }
         }
-        __syncthreads();
-    }
+    __syncthreads();
     float *mine = p.part + (size_t)blockIdx.x * 2 * p.n_pad;
-    for (int c = threadIdx.x; c < 2 * p.n_pad; c += blockDim.x) mine[c] = acc[c];
+    for (int c = threadIdx.x; c < 2 * p.n_pad; c += blockDim.x) {
+        float a = 0.0f;
+        if ((c < p.n_pad ? c : c - p.n_pad) < n)
+            for (int k = 0; k < p.groups; ++k) a += acc[(size_t)k * 2 * p.n_pad + c];
+        mine[c] = a;
+    }
 }
 
 // Rows of any length: dx by a block per row, and the column sums of a slice of rows by a block per 256 columns.

@@ -40,11 +40,7 @@ __device__ __forceinline__ int sample_of(const Params &p, long long r)     // (b
 {
     return p.rows_per_sample == 1 ? (int)r : (int)((uint32_t)r / (uint32_t)p.rows_per_sample);
 }
-__device__ __forceinline__ float row_factor(const Params &p, int s)
-{
-    const float g = __ldg(p.gamma + s);
-    return __fdiv_rn(g < 1e-5f ? 1e-5f : g, 127.0f);        // (a NaN stays one)
-}
+__device__ __forceinline__ float factor_of(float gamma) { return __fdiv_rn(gamma < 1e-5f ? 1e-5f : gamma, 127.0f); }     // (a NaN stays one)
 
 // The adapter of a sample, -1 for none.  An index that is outside the table counts as none and is reported.
 __device__ __forceinline__ int adapter_of(const Params &p, int s)
@@ -70,15 +66,17 @@ __device__ __forceinline__ float byte_float(uint32_t w, int i) { return (float)(
 // ---- few rows: inner products, a warp per (row, j) -------------------------------------------------------
 // Bound by latency: a row's A is rank x cin 16-bit values out of L2 or HBM.
 template <class H>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(1024)
 inner_rows_kernel(const Params p)
 {
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
-    const long long r = blockIdx.x;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, j = blockIdx.y * 8 + warp;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long long i = (long long)blockIdx.x * (blockDim.x >> 5) + warp, r = i / p.rank;
+    const int j = (int)(i - r * p.rank);
+    if (r >= p.m) return;
     const int a = adapter_of(p, sample_of(p, r));
-    if (a < 0 || j >= p.rank) return;
+    if (a < 0) return;
     const uint4 *x = reinterpret_cast<const uint4 *>(p.x + r * p.cin);
     const uint4 *av = reinterpret_cast<const uint4 *>(static_cast<const H *>(p.a) + ((size_t)a * p.rank + j) * p.cin);
     float sum = 0.0f;
@@ -148,9 +146,8 @@ __device__ __forceinline__ float outer(const Params &p, int a, int o, const floa
 // ---- few rows: the projection -------------------------------------------------------------------------------
 // D[16 outputs][8 rows] += W[16][32] x[32][8] with the warp-level int8 MMA: the weights' bytes, a quarter of one per
 // product, are what has to be read, and with few rows the tensor memory path has nothing to amortise its set-up on.
-// A block takes 16 MO outputs and 8 MT rows.  Latency is the bound, so its warps split K such that each has one piece of 64 PW
-// values (all of K at up to 4096 inputs) and every load of the call is on its way at once; with two pieces a warp
-// 32 rows 4096 -> 4096 took 8.0 us without adapters.
+// A block takes 16 MO outputs and 8 MT rows; its warps split K into pieces of 64 PW values.  Latency is the bound, so there
+// are as many of them as leave a piece or two to each, and what the epilogue needs beside the sums is loaded in front of them.
 // Codes become operands in three operations per 16: two's complement codes with the upper bit flipped are w + 2, and
 // (word >> 2 j) & 0x03030303 are the values k = j, 4 + j, 8 + j, 12 + j of the word's 16.  The rows' bytes are put in the same
 // order by transposing their 4 x 4 blocks, and 2 sum_k x is taken off at the end.
@@ -171,20 +168,47 @@ __device__ __forceinline__ void transpose_4x4(const uint4 &v, uint32_t (&o)[4])
     o[3] = __byte_perm(hi01, hi23, 0x7632);
 }
 
-// PW: words of 16 codes that a thread takes of each weight row.
+// PW: words of 16 codes that a thread takes of each weight row.  The four threads of a fragment's row lie side by side in
+// memory, 64 values of k apart from one word to the next.
 template <class H, class Y, int MO, int MT, int PW, int WARPS>
-__global__ void __launch_bounds__(32 * WARPS)
+__global__ void __launch_bounds__(32 * WARPS, (MT == 1 ? 2 : 1) * (WARPS == 8 ? 2 : 1))
 proj_rows_kernel(const Params p)
 {
-    __shared__ int acc_s[8][16 * MO][8 * MT + 1];
-    __shared__ int sum_s[WARPS][8 * MT];
+    constexpr int kPitch = 16 * MO + 4;         // of a row's outputs: a warp's additions fall into different banks
+    __shared__ int acc_s[8 * MT * kPitch], sum_s[8 * MT];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int o0 = blockIdx.x * 16 * MO;
     const long long r0 = (long long)blockIdx.y * 8 * MT;
     const int rowb = p.cin >> 2;
-    const bool wide = rowb % (4 * PW) == 0;
+    for (int i = threadIdx.x; i < 8 * MT * kPitch; i += 32 * WARPS) acc_s[i] = 0;
+    if (threadIdx.x < 8 * MT) sum_s[threadIdx.x] = 0;
     if (!p.chained) ptx::grid_dep_wait();
     ptx::grid_dep_launch();
+    __syncthreads();
+
+    // what an output needs beside the sums, on its way before them
+    constexpr int kEach = (128 * MO * MT + 32 * WARPS - 1) / (32 * WARPS);      // outputs of a thread
+    float alpha[kEach], gamma[kEach];
+    int a[kEach];
+    auto output = [&](int q, int &o, long long &r) {
+        const int i = threadIdx.x + q * 32 * WARPS;
+        o = o0 + i % (16 * MO);
+        r = r0 + i / (16 * MO);
+        return i < 128 * MO * MT && r < p.m && o < p.cout;
+    };
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+        int o;
+        long long r;
+        a[q] = -1;
+        alpha[q] = gamma[q] = 0.0f;
+        if (output(q, o, r)) {
+            const int s = sample_of(p, r);
+            alpha[q] = __ldg(p.alpha + o);
+            gamma[q] = __ldg(p.gamma + s);
+            a[q] = adapter_of(p, s);
+        }
+    }
 
     int d[MO][MT][4], sx[MT];
 #pragma unroll
@@ -197,7 +221,7 @@ proj_rows_kernel(const Params p)
     }
     uint32_t invalid = 0;
     for (int k0 = warp * 64 * PW; k0 < p.cin; k0 += 64 * PW * WARPS) {
-        const int k = k0 + 16 * PW * t;         // this thread's 16 PW of the piece
+        const int k = k0 + 16 * t;              // this thread's words: k, k + 64, ...
         uint32_t w[MO][2][PW];
 #pragma unroll
         for (int o = 0; o < MO; ++o)
@@ -205,29 +229,21 @@ proj_rows_kernel(const Params p)
             for (int h = 0; h < 2; ++h) {
                 const int row = o0 + 16 * o + 8 * h + g;
                 const uint8_t *src = p.w + (size_t)row * rowb + (k >> 2);
-                if (row < p.cout && wide && k < p.cin) {
-                    if constexpr (PW == 4) {
-                        const uint4 v = __ldg(reinterpret_cast<const uint4 *>(src));
-                        w[o][h][0] = v.x; w[o][h][1] = v.y; w[o][h][2] = v.z; w[o][h][3] = v.w;
-                    } else {
-                        const uint2 v = __ldg(reinterpret_cast<const uint2 *>(src));
-                        w[o][h][0] = v.x; w[o][h][1] = v.y;
-                    }
-                } else {
 #pragma unroll
-                    for (int i = 0; i < PW; ++i)
-                        w[o][h][i] = row < p.cout && k + 16 * i < p.cin ? __ldg(reinterpret_cast<const uint32_t *>(src) + i) : 0u;
-                }
+                for (int i = 0; i < PW; ++i)
+                    w[o][h][i] = row < p.cout && k + 64 * i < p.cin ? __ldg(reinterpret_cast<const uint32_t *>(src + 16 * i)) : 0u;
             }
         uint4 v[MT][PW];
 #pragma unroll
-        for (int c = 0; c < MT; ++c)
+        for (int c = 0; c < MT; ++c) {
+            const long long r = r0 + 8 * c + g;
+            const int8_t *src = p.x + r * p.cin + k;
 #pragma unroll
             for (int i = 0; i < PW; ++i) {
-                const long long r = r0 + 8 * c + g;
                 v[c][i] = make_uint4(0u, 0u, 0u, 0u);
-                if (r < p.m && k + 16 * i < p.cin) v[c][i] = __ldg(reinterpret_cast<const uint4 *>(p.x + r * p.cin + k + 16 * i));
+                if (r < p.m && k + 64 * i < p.cin) v[c][i] = __ldg(reinterpret_cast<const uint4 *>(src + 64 * i));
             }
+        }
 #pragma unroll
         for (int i = 0; i < PW; ++i) {
             uint32_t b[MT][4];
@@ -253,70 +269,37 @@ proj_rows_kernel(const Params p)
         }
     }
     if (invalid && blockIdx.y == 0) raise_status(PROM_ERR_BAD_WEIGHT);
-    // the warps' sums: those of the second eight first, added by the first eight to their own
-    auto put = [&](int slot) {
+    // B while the warps' sums are added (whole numbers: in any order)
+    Ahead ahead[kEach];
 #pragma unroll
-        for (int c = 0; c < MT; ++c)
-#pragma unroll
-            for (int o = 0; o < MO; ++o)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc_s[slot][16 * o + g + 8 * (e >> 1)][8 * c + 2 * t + (e & 1)] = d[o][c][e];
-    };
+    for (int q = 0; q < kEach; ++q) {
+        int o;
+        long long r;
+        if (a[q] >= 0 && output(q, o, r)) ahead[q].template load<H>(p, a[q], o);
+    }
 #pragma unroll
     for (int c = 0; c < MT; ++c) {
         sx[c] += __shfl_xor_sync(0xFFFFFFFFu, sx[c], 1);
         sx[c] += __shfl_xor_sync(0xFFFFFFFFu, sx[c], 2);
-        if (t == 0) sum_s[warp][8 * c + g] = sx[c];
+        if (t == 0) atomicAdd(&sum_s[8 * c + g], sx[c]);
+#pragma unroll
+        for (int o = 0; o < MO; ++o)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) atomicAdd(&acc_s[(8 * c + 2 * t + (e & 1)) * kPitch + 16 * o + g + 8 * (e >> 1)], d[o][c][e]);
     }
-    if (WARPS > 8) {
-        if (warp >= 8) put(warp - 8);
-        __syncthreads();
-        if (warp < 8) {
-#pragma unroll
-            for (int c = 0; c < MT; ++c)
-#pragma unroll
-                for (int o = 0; o < MO; ++o)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) d[o][c][e] += acc_s[warp][16 * o + g + 8 * (e >> 1)][8 * c + 2 * t + (e & 1)];
-            __syncwarp();
-        }
-    }
-    if (warp < 8) put(warp);
     __syncthreads();
-    constexpr int kEach = (128 * MO * MT + 32 * WARPS - 1) / (32 * WARPS);      // outputs of a thread
-    float y[kEach], f[kEach];
-    int a[kEach];
-    Ahead ahead[kEach];
-#pragma unroll
-    for (int q = 0; q < kEach; ++q) {
-        const int i = threadIdx.x + q * 32 * WARPS, o = i % (16 * MO), c = i / (16 * MO);
-        const long long r = r0 + c;
-        a[q] = -1;
-        y[q] = f[q] = 0.0f;
-        if (c >= 8 * MT || r >= p.m || o0 + o >= p.cout) continue;
-        int acc = 0, sum = 0;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) acc += acc_s[w][o][c];
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) sum += sum_s[w][c];
-        const int s = sample_of(p, r);
-        f[q] = row_factor(p, s);
-        y[q] = (float)(acc - 2 * sum) * __ldg(p.alpha + o0 + o) * f[q];
-        a[q] = adapter_of(p, s);
-        if (a[q] >= 0) {
-            if (p.scale) f[q] *= __ldg(p.scale + a[q]);
-            ahead[q].template load<H>(p, a[q], o0 + o);
-        }
-    }
     if (p.chained) ptx::grid_dep_wait();        // for the inner products
     bool bad = false;
 #pragma unroll
     for (int q = 0; q < kEach; ++q) {
-        const int i = threadIdx.x + q * 32 * WARPS, o = i % (16 * MO), c = i / (16 * MO);
-        const long long r = r0 + c;
-        if (c >= 8 * MT || r >= p.m || o0 + o >= p.cout) continue;
-        if (a[q] >= 0) y[q] += f[q] * outer<H>(p, a[q], o0 + o, p.t + r * p.rank, ahead[q], bad);
-        static_cast<Y *>(p.y)[r * p.y_pitch + o0 + o] = norm::from_float<Y>(y[q]);
+        int o;
+        long long r;
+        if (!output(q, o, r)) continue;
+        const int c = (int)(r - r0), acc = acc_s[c * kPitch + o - o0] - 2 * sum_s[c];
+        const float f = factor_of(gamma[q]);
+        float y = (float)acc * alpha[q] * f;
+        if (a[q] >= 0) y += (p.scale ? __ldg(p.scale + a[q]) * f : f) * outer<H>(p, a[q], o, p.t + r * p.rank, ahead[q], bad);
+        static_cast<Y *>(p.y)[r * p.y_pitch + o] = norm::from_float<Y>(y);
     }
     if (bad) raise_status(PROM_ERR_BAD_WEIGHT);
 }
@@ -943,7 +926,7 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
             bool with = false;
             if (r < p.m) {
                 const int s = sample_of(p, r);
-                fac = row_factor(p, s);
+                fac = factor_of(__ldg(p.gamma + s));
                 if (adapters) {
                     const int a = __ldcg(p.row_adapter + r);
                     with = a >= 0;

@@ -2442,24 +2442,43 @@ static prom_status launch_rows(const Params &p, cudaStream_t st)
     return cuda_status(e);
 }
 
-// Warps and words such that K is one piece per warp, as long as a block has an SM to itself; smaller blocks, of which two
-// share an SM, where there are more (64 rows 4096 -> 4096: 14.7 us, 19.4 with sixteen warps).
-template <class H, class Y, int MO, int MT>
-static prom_status launch_rows_for(const Params &p, const DeviceInfo &d, cudaStream_t st)
+// A block to an SM and sixteen warps to a block while there are no more blocks than SMs, else two blocks of eight (64 rows
+// 4096 -> 4096, 8 adapters of rank 16: 14.2 us, 16.1 with sixteen warps).
+static bool one_block_each(const Params &p, const DeviceInfo &d)
 {
-    const long long blocks = (long long)((p.cout + 16 * MO - 1) / (16 * MO)) * ((p.m + 8 * MT - 1) / (8 * MT));
-    if (p.cin <= 1024) return launch_rows<H, Y, MO, MT, 2, 8>(p, st);
-    if (MT > 1 && blocks > d.sms) return launch_rows<H, Y, MO, MT, 4, 8>(p, st);
-    if (p.cin <= 2048) return launch_rows<H, Y, MO, MT, 2, 16>(p, st);
-    return launch_rows<H, Y, MO, MT, 4, 16>(p, st);
+    return p.cin > 1024 && (long long)((p.cout + 31) / 32) * ((p.m + 31) / 32) <= d.sms;
+}
+
+template <class H, class Y>
+static prom_status run_rows(Params &p, const DeviceInfo &d, cudaStream_t st)
+{
+    const bool few = p.m <= 8, one_each = one_block_each(p, d);
+    if (p.a) {
+        cudaLaunchConfig_t cfg;
+        cudaLaunchAttribute attr[1];
+        // Beside projection blocks that fill an SM's registers the inner products keep to few SMs, so that those start at once
+        // (32 rows 4096 -> 4096, rank 16: 9.1 us, 11.4 with blocks of eight warps); otherwise they spread.
+        const int warps = !few && one_each ? 32 : 8;
+        fill_launch_cfg(cfg, attr, (int)((p.m * p.rank + warps - 1) / warps), 32 * warps, 0, st, true);
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, inner_rows_kernel<H>, p);
+        ++g_launches;
+        if (e != cudaSuccess) return cuda_status(e);
+        p.chained = 1;
+    }
+    if (few) {
+        if (p.cin <= 1024) return launch_rows<H, Y, 1, 1, 2, 8>(p, st);
+        return p.cin <= 2048 ? launch_rows<H, Y, 1, 1, 2, 16>(p, st) : launch_rows<H, Y, 1, 1, 4, 16>(p, st);
+    }
+    return one_each ? launch_rows<H, Y, 2, 4, 2, 16>(p, st) : launch_rows<H, Y, 2, 4, 2, 8>(p, st);
 }
 
 // Which kernels: microseconds of both, fitted to timings of 1 to 512 rows (384 -> 576, 960 -> 1280, 1024 -> 4096, 2048 -> 2048,
 // 4096 -> 4096; graph replays, 8 adapters of rank 16 and none).  The first cost their blocks of 32 rows x 32 outputs, the
-// tiled ones whole passes over K.  Measured at 960 -> 1280 with adapters, rows / tiles: 128 rows 9.6 / 15.8, 256 rows
-// 15.5 / 16.1, 512 rows 24.4 / 15.3; at 4096 -> 4096: 64 rows 14.7 / 23.4, 128 rows 26.6 / 24.6.  Inner products cost
-// the first per row and rank, the tiled ones per adapter that a tile of rows may have (416 -> 2576, 181 rows, 16 adapters:
-// 13.9 / 26.2; 80 -> 40, 672 rows, one adapter of rank 32: 13.6 / 11.1).
+// tiled ones whole passes over K.  Measured at 960 -> 1280 with adapters, rows / tiles: 128 rows 8.5 / 16.0, 256 rows
+// 14.0 / 16.2, 512 rows 22.1 / 15.2; at 4096 -> 4096: 64 rows 14.2 / 23.5, 128 rows 25.6 / 24.2; without adapters 64 rows
+// 9.7 / 13.4, 96 rows 14.8 / 13.6.  Inner products cost the first per row and rank, the tiled ones per adapter that a tile
+// of rows may have (416 -> 2576, 181 rows, 16 adapters: 13.7 / 23.5; 80 -> 40, 672 rows, one adapter of rank 32:
+// 13.3 / 10.6).
 static bool rows_faster(const Params &p, int pairs)
 {
     if (p.m > 65535ll * 32) return false;
@@ -2468,29 +2487,12 @@ static bool rows_faster(const Params &p, int pairs)
     int nt = 256;
     while (nt > 64 && mtiles * ((p.cout + nt - 1) / nt) < pairs) nt /= 2;
     const double waves = (double)((mtiles * ((p.cout + nt - 1) / nt) + pairs - 1) / pairs);
-    if (!p.a) return 3.0 + blocks * (0.014 + 3.5e-6 * k) <= 3.0 + waves * (1.5 + 0.0022 * k * nt / 64);
+    if (!p.a) return 2.6 + blocks * (0.0043 + 6e-6 * k) <= 3.1 + waves * (1.3 + 0.0022 * k * nt / 64);
     const long long samples = (p.m + p.rows_per_sample - 1) / p.rows_per_sample, in_tile = (kTile - 1) / p.rows_per_sample + 1;
     const long long adapters = std::min<long long>(p.n, std::min(samples, in_tile));
     const double rows = 6.0 + blocks * (0.022 + 5e-6 * k) + 2.8e-4 * (double)p.m * p.rank;
     const double tiles = 12.5 + waves * (2.0 + 0.0022 * k * nt / 64 + 0.5 * (double)(adapters * ((2 * p.rank + 63) / 64)));
     return rows <= tiles;
-}
-
-template <class H, class Y>
-static prom_status run_rows(Params &p, const DeviceInfo &d, cudaStream_t st)
-{
-    if (p.a) {
-        cudaLaunchConfig_t cfg;
-        cudaLaunchAttribute attr[1];
-        fill_launch_cfg(cfg, attr, 1, 256, 0, st, true);
-        cfg.gridDim = dim3((unsigned)p.m, (unsigned)((p.rank + 7) / 8));
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, inner_rows_kernel<H>, p);
-        ++g_launches;
-        if (e != cudaSuccess) return cuda_status(e);
-        p.chained = 1;
-    }
-    if (p.m <= 8) return launch_rows_for<H, Y, 1, 1>(p, d, st);
-    return launch_rows_for<H, Y, 2, 4>(p, d, st);
 }
 
 // Pairs of CTAs of the tiled kernel that the device holds at once.

@@ -75,6 +75,33 @@ template <> __device__ __forceinline__ float half_of<float>(uint32_t w, int) { r
 
 template <class T> constexpr int kWide = 16 / (int)sizeof(T);      // elements of a 16-byte access
 
+// Two neighbours in one operation each, rounded as two single ones would be: the kernels' issue slots, and not the operations
+// themselves, are what runs short beside the memory (backward, 16384 x 4096 bf16: 84.1 us one value at a time, 80.5 so).
+struct Two { float x, y; };
+__device__ __forceinline__ Two both(float v) { return {v, v}; }
+__device__ __forceinline__ Two operator+(Two a, Two b)
+{
+    Two d;
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ Two operator*(Two a, Two b)
+{
+    Two d;
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ Two fma_of(Two a, Two b, Two c)
+{
+    Two d;
+    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 d, a, b, c;\n"
+        "mov.b64 {%0, %1}, d;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+
 template <class T, int E> struct Piece {
     uint4 raw;
     __device__ __forceinline__ Piece() : raw(make_uint4(0u, 0u, 0u, 0u)) {}
@@ -91,6 +118,7 @@ template <class T, int E> struct Piece {
         const uint32_t w = i == 0 ? raw.x : i == 1 ? raw.y : i == 2 ? raw.z : raw.w;
         return sizeof(T) == 4 ? __uint_as_float(w) : half_of<T>(w, e & 1);
     }
+    __device__ __forceinline__ Two two(int e) const { return {get(e), get(e + 1)}; }
     __device__ __forceinline__ void set(const float (&f)[E])
     {
         if constexpr (sizeof(T) == 4) raw = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
@@ -139,6 +167,16 @@ template <class T> struct Piece<T, 1> {
     __device__ __forceinline__ void set(const float (&f)[1]) { v = from_float<T>(f[0]); }
     __device__ __forceinline__ void again() {}
 };
+
+// One value or two, for kernels of both kinds of pieces.
+template <class P> __device__ __forceinline__ P all(float v) { if constexpr (sizeof(P) == 8) return both(v); else return v; }
+template <class P, class T, int E> __device__ __forceinline__ P some(const Piece<T, E> &v, int e) { if constexpr (sizeof(P) == 8) return v.two(e); else return v.get(e); }
+template <class P> __device__ __forceinline__ P some(const float *f, int e) { if constexpr (sizeof(P) == 8) return {f[e], f[e + 1]}; else return f[e]; }
+__device__ __forceinline__ void put(float *f, int e, Two v) { f[e] = v.x; f[e + 1] = v.y; }
+__device__ __forceinline__ void put(float *f, int e, float v) { f[e] = v; }
+__device__ __forceinline__ float sum_of(Two v) { return v.x + v.y; }
+__device__ __forceinline__ float sum_of(float v) { return v; }
+__device__ __forceinline__ float fma_of(float a, float b, float c) { return fmaf(a, b, c); }
 
 // A vector of parameters (weight or bias) of any of the types; absent: `otherwise`.
 struct Vector {
@@ -556,51 +594,68 @@ forward_groups_kernel(const Fwd p)
 }
 
 // ---- forward: a warp per short row ----------------------------------------------------------------------------
-// V pieces a lane, in registers; the parameters in shared memory as in the next kernel.  (A bulk copy of a row of a
-// kilobyte costs more than its loads: 25088 x 192 float32, 14.3 us through shared memory, 11.5 here.)
+// V pieces a lane, in registers, and with up to two the next row's too (25088 x 192 float32 9.8 us, 11.3 without; 16384 x 1024
+// float16, where four run out of registers, 16.6, 14.2 without); the parameters in shared memory as in the next kernel.  (A bulk
+// copy of a row of a kilobyte costs more than its loads: 25088 x 192 float32, 14.3 us through shared memory.)
 template <class T, int V, bool CODES>
 __global__ void __launch_bounds__(1024, 1)
 forward_short_kernel(const Fwd p)
 {
     using Sum = typename std::conditional<CODES, double, float>::type;
     constexpr int E = kWide<T>;
+    constexpr bool kAhead = V <= 2;
     extern __shared__ __align__(16) float short_params[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = p.n, m = (int)p.m, pieces = n / E;
     float *sw = short_params, *sb = short_params + n;
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
+    const Sum inv_n = (Sum)1 / (Sum)n;
+    Piece<T, E> next[V];
+    auto load = [&](long long r) {
+        const T *row = static_cast<const T *>(p.x) + r * p.x_pitch;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (r < m && lane + 32 * i < pieces) next[i].load(row + (lane + 32 * i) * E);
+    };
+    if constexpr (kAhead) load((long long)warp * gridDim.x + blockIdx.x);
     stage_parameters<E>(p, sw, sb);
     __syncthreads();
-    const Sum inv_n = (Sum)1 / (Sum)n;
 #pragma unroll 1
     for (long long r = (long long)warp * gridDim.x + blockIdx.x; r < m; r += 32ll * gridDim.x) {
-        const T *row = static_cast<const T *>(p.x) + r * p.x_pitch;
         Piece<T, E> v[V];
+        if constexpr (!kAhead) load(r);
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (lane + 32 * i < pieces) v[i].load(row + (lane + 32 * i) * E);
+        for (int i = 0; i < V; ++i) v[i] = next[i];
+        if constexpr (kAhead) load(r + 32ll * gridDim.x);
         Sum s = 0;
+        Two t = both(0.0f);
 #pragma unroll
         for (int i = 0; i < V; ++i)
 #pragma unroll
-            for (int e = 0; e < E; ++e) {   // (what lies past the row is zero)
-                if constexpr (CODES) s = fma(scaled_down<T>(v[i].get(e)), two_896(), s);
-                else s += v[i].get(e);
+            for (int e = 0; e < E; e += 2) {    // (what lies past the row is zero)
+                if constexpr (CODES) s = fma(scaled_down<T>(v[i].get(e + 1)), two_896(), fma(scaled_down<T>(v[i].get(e)), two_896(), s));
+                else t = t + v[i].two(e);
             }
+        if constexpr (!CODES) s = t.x + t.y;
         const Sum mean = warp_sum(s) * inv_n;
         s = 0;
+        t = both(0.0f);
 #pragma unroll
         for (int i = 0; i < V; ++i)
             if (lane + 32 * i < pieces) {
                 v[i].again();
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    Sum d;
-                    if constexpr (CODES) d = fma(scaled_down<T>(v[i].get(e)), two_896(), -mean);
-                    else d = v[i].get(e) - mean;
-                    s = fma(d, d, s);
+                for (int e = 0; e < E; e += 2) {
+                    if constexpr (CODES) {
+                        const double d = fma(scaled_down<T>(v[i].get(e)), two_896(), -mean), d2 = fma(scaled_down<T>(v[i].get(e + 1)), two_896(), -mean);
+                        s = fma(d2, d2, fma(d, d, s));
+                    } else {
+                        const Two d = v[i].two(e) + both(-mean);
+                        t = fma_of(d, d, t);
+                    }
                 }
             }
+        if constexpr (!CODES) s = t.x + t.y;
         float mu = (float)mean, rstd = (float)inverse_root(warp_sum(s) * inv_n + (Sum)p.eps);
         if constexpr (!CODES) {
             T *out = static_cast<T *>(p.y) + r * p.y_pitch;
@@ -611,7 +666,11 @@ forward_short_kernel(const Fwd p)
                     parameters_of<E>(sw, sb, pieces, lane + 32 * i, w, b);
                     v[i].again();
 #pragma unroll
-                    for (int e = 0; e < E; ++e) w[e] = (v[i].get(e) - mu) * rstd * w[e] + b[e];
+                    for (int e = 0; e < E; e += 2) {
+                        const Two y = fma_of((v[i].two(e) + both(-mu)) * both(rstd), Two{w[e], w[e + 1]}, Two{b[e], b[e + 1]});
+                        w[e] = y.x;
+                        w[e + 1] = y.y;
+                    }
                     v[i].set(w);
                     v[i].store(out + (lane + 32 * i) * E);
                 }
@@ -647,7 +706,7 @@ forward_short_kernel(const Fwd p)
 // For many rows of whole pieces.  No exchange between warps, and what belongs to a row worked out once for all of it.  A bulk
 // copy brings the row into shared memory, where the warp passes over it three times (four for codes): in registers the
 // longer rows leave none for the arithmetic.  As many warps as there is room for rows; while one waits for its row the
-// others work.
+// others work, and the row behind comes to L2 meanwhile (8192 x 4096 bf16 31.1 us, 33.9 without; to codes 42.3, 45.7).
 template <class T, bool CODES>
 __global__ void __launch_bounds__(1024, 1)
 forward_warps_kernel(const Fwd p)
@@ -687,9 +746,11 @@ forward_warps_kernel(const Fwd p)
                 if (failed || ptx::globaltimer() - t0 > actq::kWaitLimitNs) { failed = 1; break; }
         }
         if (__any_sync(0xFFFFFFFFu, failed)) break;
+        if (lane == 0 && r + warps < m) ptx::bulk_prefetch(x + (r + warps) * p.x_pitch, row_bytes);
         Piece<T, E> v;
         Sum s = 0, s2 = 0;
         [[maybe_unused]] Sum sq = 0, sq2 = 0;
+        Two t = both(0.0f);
 #pragma unroll 4
         for (int i = lane; i < pieces; i += 32) {
             v.raw = mine[i];
@@ -702,11 +763,11 @@ forward_warps_kernel(const Fwd p)
                     sq = fma(d, d, sq);
                     sq2 = fma(d2, d2, sq2);
                 } else {
-                    s += v.get(e);
-                    s2 += v.get(e + 1);
+                    t = t + v.two(e);
                 }
             }
         }
+        if constexpr (!CODES) s = t.x + t.y;
         const Sum mean = warp_sum(s + s2) * inv_n;
         // In 64 bits the squares of the values (exact there) can be summed on the same pass: what their difference to the mean's
         // square loses is seen, and where it is more than twelve bits the differences are taken after all.
@@ -718,23 +779,23 @@ forward_warps_kernel(const Fwd p)
         }
         if (again) {
             s = s2 = 0;
+            t = both(0.0f);
 #pragma unroll 4
             for (int i = lane; i < pieces; i += 32) {
                 v.raw = mine[i];
 #pragma unroll
                 for (int e = 0; e < E; e += 2) {
-                    Sum d, d2;
                     if constexpr (CODES) {
-                        d = fma(scaled_down<T>(v.get(e)), two_896(), -mean);
-                        d2 = fma(scaled_down<T>(v.get(e + 1)), two_896(), -mean);
+                        const double d = fma(scaled_down<T>(v.get(e)), two_896(), -mean), d2 = fma(scaled_down<T>(v.get(e + 1)), two_896(), -mean);
+                        s = fma(d, d, s);
+                        s2 = fma(d2, d2, s2);
                     } else {
-                        d = v.get(e) - mean;
-                        d2 = v.get(e + 1) - mean;
+                        const Two d = v.two(e) + both(-mean);
+                        t = fma_of(d, d, t);
                     }
-                    s = fma(d, d, s);
-                    s2 = fma(d2, d2, s2);
                 }
             }
+            if constexpr (!CODES) s = t.x + t.y;
             var = warp_sum(s + s2) * inv_n;
         }
         float mu = (float)mean, rstd = (float)inverse_root(var + (Sum)p.eps);
@@ -746,7 +807,11 @@ forward_warps_kernel(const Fwd p)
                 parameters(i, w, b);
                 v.raw = mine[i];
 #pragma unroll
-                for (int e = 0; e < E; ++e) w[e] = (v.get(e) - mu) * rstd * w[e] + b[e];
+                for (int e = 0; e < E; e += 2) {
+                    const Two y = fma_of((v.two(e) + both(-mu)) * both(rstd), Two{w[e], w[e + 1]}, Two{b[e], b[e + 1]});
+                    w[e] = y.x;
+                    w[e + 1] = y.y;
+                }
                 v.set(w);
                 v.store(out + i * E);
             }
@@ -990,6 +1055,8 @@ backward_kernel(const Bwd p)
     constexpr int R = kBwdRows<V, RING>;
     constexpr bool kShift = !RING && E > 1;     // rows may start anywhere
     constexpr bool kHoldW = V * E <= 16;
+    constexpr int kStep = E > 1 ? 2 : 1;
+    using Some = typename std::conditional<(E > 1), Two, float>::type;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t bars[RING ? kMaxGroups * kMaxStages : 1];
     __shared__ float4 red[2][32];
@@ -1098,22 +1165,24 @@ backward_kernel(const Bwd p)
         }
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            s1[k] = s2[k] = 0.0f;
+            Some t1 = all<Some>(0.0f), t2 = t1;
 #pragma unroll
             for (int i = 0; i < V; ++i)
                 if (in_row(i)) {
                     float w[E];
                     if constexpr (!kHoldW) p.w.get_at<E>(c0 + i * hop, n, 1.0f, w);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {       // (a row that is not there is one of zeros, as is dy outside a row)
-                        const float we = kHoldW ? held[kHoldW ? i : 0][e] : w[e];
-                        const float d = vd[k][i].get(e), xh = (vx[k][i].get(e) - mean[k]) * rstd[k], gr = d * we;
-                        s1[k] += gr;
-                        s2[k] += gr * xh;
-                        dw[i][e] += d * xh;
-                        db[i][e] += d;
+                    for (int e = 0; e < E; e += kStep) {       // (a row that is not there is one of zeros, as is dy outside a row)
+                        const Some we = some<Some>(kHoldW ? held[kHoldW ? i : 0] : w, e);
+                        const Some d = some<Some>(vd[k][i], e), xh = (some<Some>(vx[k][i], e) + all<Some>(-mean[k])) * all<Some>(rstd[k]), gr = d * we;
+                        t1 = t1 + gr;
+                        t2 = fma_of(gr, xh, t2);
+                        put(dw[i], e, fma_of(d, xh, some<Some>(dw[i], e)));
+                        put(db[i], e, some<Some>(db[i], e) + d);
                     }
                 }
+            s1[k] = sum_of(t1);
+            s2[k] = sum_of(t2);
         }
         float v = R == 2 ? warp_sum_4(s1[0], s2[0], s1[R - 1], s2[R - 1]) : warp_sum_2(s1[0], s2[0]);
         constexpr int kValues = 2 * R, kSpan = 32 / kValues;
@@ -1154,10 +1223,10 @@ backward_kernel(const Bwd p)
                             vx[k][i].again();
                             vd[k][i].again();
 #pragma unroll
-                            for (int e = 0; e < E; ++e) {
-                                const float we = kHoldW ? held[kHoldW ? i : 0][e] : w[e];
-                                const float xh = (vx[k][i].get(e) - mean[k]) * rstd[k];
-                                w[e] = rstd[k] * (vd[k][i].get(e) * we - s1[k] - xh * s2[k]);
+                            for (int e = 0; e < E; e += kStep) {
+                                const Some we = some<Some>(kHoldW ? held[kHoldW ? i : 0] : w, e);
+                                const Some xh = (some<Some>(vx[k][i], e) + all<Some>(-mean[k])) * all<Some>(rstd[k]);
+                                put(w, e, all<Some>(rstd[k]) * fma_of(xh, all<Some>(-s2[k]), fma_of(some<Some>(vd[k][i], e), we, all<Some>(-s1[k]))));
                             }
                             Piece<T, E> o;
                             o.set(w);

@@ -155,6 +155,12 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *gsrc, uint32
                  : "memory");
 }
 
+// Asks for `bytes` (a multiple of 16, from a 16-byte boundary) to be brought into L2.
+__device__ __forceinline__ void bulk_prefetch(const void *src, uint32_t bytes)
+{
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" :: "l"(__cvta_generic_to_global(src)), "r"(bytes) : "memory");
+}
+
 // ---- copies of a few bytes per thread into shared memory, and 16-byte stores --------------------------
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void *src)
 {

@@ -495,7 +495,8 @@ prom_status prom_pw_conv_i8_addsub_static(const int8_t *x_dev, int64_t m, int ci
 
 /* Synchronises `cuda_stream`, then returns and clears the device status word:
  * PROM_OK, PROM_ERR_BAD_REQUANT, PROM_ERR_BAD_WEIGHT (invalid 2-bit code met
- * by a kernel) or PROM_ERR_TIMEOUT. */
+ * by a kernel, a value of an adapter's B that is not finite), PROM_ERR_RANGE (an
+ * index outside its table) or PROM_ERR_TIMEOUT. */
 prom_status prom_last_device_status(void *cuda_stream);
 
 /* Number of kernels this library has launched since it was loaded (all

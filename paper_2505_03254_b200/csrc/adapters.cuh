@@ -64,7 +64,8 @@ template <> __device__ __forceinline__ float2 unpack_2<__half>(uint32_t w) { ret
 __device__ __forceinline__ float byte_float(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
 
 // ---- few rows: inner products, a warp per (row, j) -------------------------------------------------------
-// Bound by latency: a row's A is rank x cin 16-bit values out of L2 or HBM.
+// Bound by latency: a row's A is rank x cin 16-bit values out of L2 or HBM (32 rows 4096 -> 4096, rank 16: the call takes 9.2 us
+// with the kernel below, that one alone 5.9; their bytes, 2 us).
 template <class H>
 __global__ void __launch_bounds__(1024)
 inner_rows_kernel(const Params p)
@@ -598,6 +599,9 @@ inner_tiles_kernel(const Params p)
 // x comes by TMA.  The weights never exist as bytes in memory: eight warps expand the 2-bit codes into the swizzled
 // operand layout on their way into shared memory (four pairs of warps take the stages in turn), so a stage takes 4 KB of weights from L2 instead of 16 (a pair's SM would
 // need 64 bytes a clock of both operands at the MMAs' rate, of the 58 that L2 gives it; this way it is 40).
+// 8192 rows 4096 -> 4096 with adapters of rank 64 take 169 us, of which the inner products in front take 29; without adapters 103
+// (2.7 POPS of 4.56): the tensor pipe is busy 55 % of the time, since the accumulators fill the tensor memory and a tile's
+// read-out has no MMAs beside it.
 // Behind the chunks of K come those of the adapters: for each adapter of the tile the rows' inner products (zero for rows of
 // other adapters), as sums of 16-bit values (two, or three for binary32 outputs) side by side along K, against B
 // repeated as often.

@@ -2302,8 +2302,8 @@ static prom_status run_forward(Fwd &p, bool wide, const DeviceInfo &d, cudaStrea
     // one more piece than the row fills, where it starts inside one
     const int pieces = p.period ? (p.n + (p.period > 1 || !wide ? E - 1 : 0) + E - 1) / E : 0;
     // Many rows: a warp each, out of registers up to 128 pieces (64 for codes), out of shared memory while about a dozen rows
-    // fit there (us, warps / blocks: 8192 x 4096 bf16 38 / 47, to codes 54 / 72; 4096 x 8192 bf16 53 / 38, to codes 71 / 63;
-    // 8192 x 4096 float32 61 / 49, to codes 64 / 95).
+    // fit there (us, warps / blocks: 16384 x 4096 bf16 53 / 70, 8192 x 4096 to codes 42 / 52; 4096 x 8192 bf16 49 / 38, to codes
+    // 62 / 60; 8192 x 4096 float32 57 / 49, to codes 55 / 74).
     if (wide && p.m >= 8ll * d.sms) {
         const int whole = p.n / E;
         if (whole <= 32) return launch_short<T, 1, CODES>(p, d, st);

@@ -595,13 +595,16 @@ inner_tiles_kernel(const Params p)
 
 // ---- many rows: the projection -------------------------------------------------------------------------------------
 // Tiles of 256 rows x nt outputs by pairs of CTAs (cta_group::2, 128 rows of x and half of the tile's weights in each),
-// two accumulators in tensor memory: int32 for the projection, binary32 for the adapters, which the epilogue joins.
+// accumulators of two kinds in tensor memory: int32 for the projection, binary32 for the adapters, which the epilogue joins;
+// two of each where they fit (without adapters, and up to 128 outputs), so that a tile is read out beside the next one's MMAs.
 // x comes by TMA.  The weights never exist as bytes in memory: eight warps expand the 2-bit codes into the swizzled
-// operand layout on their way into shared memory (four pairs of warps take the stages in turn), so a stage takes 4 KB of weights from L2 instead of 16 (a pair's SM would
-// need 64 bytes a clock of both operands at the MMAs' rate, of the 58 that L2 gives it; this way it is 40).
-// 8192 rows 4096 -> 4096 with adapters of rank 64 take 169 us, of which the inner products in front take 29; without adapters 103
-// (2.7 POPS of 4.56): the tensor pipe is busy 55 % of the time, since the accumulators fill the tensor memory and a tile's
-// read-out has no MMAs beside it.
+// operand layout on their way into shared memory (four pairs of warps take the stages in turn), so a stage takes 4 KB of
+// weights from L2 instead of 16 (a pair's SM would need 64 bytes a clock of both operands at the MMAs' rate, of the 58 that L2
+// gives it; this way it is 40).
+// 8192 rows 4096 -> 4096 with adapters of rank 64 take 142 us, of which the inner products in front take 29; without adapters 98
+// (2.8 POPS of 4.56).  Bound by the stages' rate, 0.4 us each where their MMAs take 0.3: narrower tiles with two accumulators of
+// each kind take longer (160 outputs 201 us, 128 outputs 223, when 256 took 154), and twice as many fillers on half as
+// many epilogue warps gain 2 % there and lose 10 % at 1024 -> 4096.
 // Behind the chunks of K come those of the adapters: for each adapter of the tile the rows' inner products (zero for rows of
 // other adapters), as sums of 16-bit values (two, or three for binary32 outputs) side by side along K, against B
 // repeated as often.
@@ -609,18 +612,26 @@ constexpr int kFillGroups = 4, kGroupWarps = 2, kFillWarps = kFillGroups * kGrou
 constexpr int kEpiGroups = 4, kEpiWarps = 4 * kEpiGroups;
 constexpr int kFill0 = 2, kEpi0 = kFill0 + kFillWarps;
 constexpr int kTileThreads = 32 * (kEpi0 + kEpiWarps);
-constexpr int kStages = 4;
 constexpr uint32_t kHalfStage = 128u * 128u, kStage = 2u * kHalfStage;      // rows of x, rows of weights: 128 bytes of K each
-constexpr uint32_t kSlab = 32u * 128u;                                      // an epilogue warp's 32 rows x 32 outputs
-constexpr uint32_t kOffSlab = kStages * kStage;
-constexpr uint32_t kOffBars = kOffSlab + kEpiWarps * kSlab;
-constexpr size_t kTileSmem = 1024 + kOffBars + 256;
-constexpr uint32_t kD2 = 256;               // column of the adapters' accumulator
+// As many stages as fit beside the epilogue warps' slabs of 32 rows x 32 outputs.  A group of fillers that has entered a stage
+// knows that the one kStages before it is done: its next one, kFillGroups further, must not lie a whole round beyond that,
+// or its wait could not tell the phase before from the one it needs.
+template <class Y> struct TileLayout {
+    static constexpr int kStages = sizeof(Y) == 4 ? 5 : 6;
+    static constexpr uint32_t kSlab = 32u * 32u * (uint32_t)sizeof(Y);
+    static constexpr uint32_t kOffSlab = kStages * kStage;
+    static constexpr uint32_t kOffBars = kOffSlab + kEpiWarps * kSlab;
+    static constexpr size_t kSmem = 1024 + kOffBars + 256;
+    static_assert(kFillGroups <= kStages, "waits of the fillers");
+    static_assert(kSmem <= 227 * 1024, "shared memory");
+};
 
 struct Tiles {
     Params p;
     int kc, ksteps_last;        // chunks of 128 bytes of K; MMA steps in the last one
     int n_mtiles, n_ctiles, nt;
+    int depth;                  // the projection's accumulators, nt columns each (the adapters' behind them)
+    int d2_step;                // from one of the adapters' to the next; 0: there is one
     int store;                  // y has a tensor map
 };
 
@@ -637,6 +648,7 @@ template <class H, class Y>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kTileThreads, 1)
 proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap, const Tiles q)
 {
+    constexpr int kStages = TileLayout<Y>::kStages;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (ptx::smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t base = ptx::smem_u32(smem);
@@ -646,11 +658,11 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
 
     // In the first CTA: full (its loader's arrival, both CTAs' fillers and both loads' bytes) and tempty (both read-outs).
     // In each: empty and tfull, by the MMAs' completion.
-    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + kOffBars);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + TileLayout<Y>::kOffBars);
     const uint32_t bar_full = ptx::smem_u32(bars), bar_empty = bar_full + 8 * kStages;
-    const uint32_t bar_tfull = bar_empty + 8 * kStages, bar_tempty = bar_tfull + 8, bar_drain = bar_tempty + 8;
-    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(bars + 2 * kStages + 3);
-    volatile int *flags = reinterpret_cast<volatile int *>(bars + 2 * kStages + 4);
+    const uint32_t bar_tfull = bar_empty + 8 * kStages, bar_tempty = bar_tfull + 16, bar_drain = bar_tempty + 16;      // (two accumulators)
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(bars + 2 * kStages + 5);
+    volatile int *flags = reinterpret_cast<volatile int *>(bars + 2 * kStages + 6);
 
     const int pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
     const long long units = (long long)q.n_mtiles * q.n_ctiles;
@@ -662,8 +674,10 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
             ptx::mbar_init(bar_full + 8 * lane, 1 + 2 * kFillWarps);
             ptx::mbar_init(bar_empty + 8 * lane, 1);
         } else if (lane == 31) {
-            ptx::mbar_init(bar_tfull, 1);
-            ptx::mbar_init(bar_tempty, 2 * kEpiWarps);
+            for (int i = 0; i < 2; ++i) {
+                ptx::mbar_init(bar_tfull + 8 * i, 1);
+                ptx::mbar_init(bar_tempty + 8 * i, 2 * kEpiWarps);
+            }
             ptx::mbar_init(bar_drain, 1);
             flags[0] = 0;
             ptx::tma_prefetch_desc(&xmap);
@@ -724,11 +738,15 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
             uint32_t st = 0, ph = 0, done = 0;
             bool ok = true, waited = !p.chained;
             auto wait_full = [&] { return tc::wait_bar_warp(bar_full + 8 * st, ph, flags); };
+            // for the read-out of the `n`-th unit of an accumulator, counted from 1 (0: returns at once)
+            auto wait_read = [&](uint32_t buf, uint32_t n) { return tc::wait_bar_warp(bar_tempty + 8 * buf, (n & 1u) ^ 1u, flags); };
             for (long long u = pair; u < units && ok; u += pairs, ++done) {
                 const int mt = (int)(u / q.n_ctiles), ct = (int)(u % q.n_ctiles);
                 const uint32_t shape = (((uint32_t)width(ct) >> 3) << 17) | ((256u >> 4) << 24);
                 const uint32_t id_i8 = (2u << 4) | (1u << 7) | (1u << 10) | shape, id_f16 = (1u << 4) | f16_types | shape;
-                if (!tc::wait_bar_warp(bar_tempty, (done & 1u) ^ 1u, flags)) { ok = false; break; }
+                const uint32_t buf = q.depth == 2 ? done & 1u : 0u, use = q.depth == 2 ? done >> 1 : done;
+                const uint32_t d1 = tmem + buf * (uint32_t)q.nt, d2 = tmem + (uint32_t)(q.depth * q.nt) + buf * (uint32_t)q.d2_step;
+                if (!wait_read(buf, use)) { ok = false; break; }
                 ptx::tc_fence_after_sync();
                 for (int c = 0; c < q.kc; ++c) {
                     if (!wait_full()) { ok = false; break; }
@@ -736,12 +754,12 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                     const uint32_t a_lo = a_lo0 + st * step, b_lo = a_lo + half;
                     const int nks = c == q.kc - 1 ? q.ksteps_last : 4;
                     if (leader) {
-                        if (c == 0) ptx::mma_i8_pair<false>(tmem, d_128 | (uint64_t)a_lo, d_128 | (uint64_t)b_lo, id_i8);
-                        else ptx::mma_i8_pair<true>(tmem, d_128 | (uint64_t)a_lo, d_128 | (uint64_t)b_lo, id_i8);
+                        if (c == 0) ptx::mma_i8_pair<false>(d1, d_128 | (uint64_t)a_lo, d_128 | (uint64_t)b_lo, id_i8);
+                        else ptx::mma_i8_pair<true>(d1, d_128 | (uint64_t)a_lo, d_128 | (uint64_t)b_lo, id_i8);
 #pragma unroll
                         for (int ks = 1; ks < 4; ++ks)
                             if (ks < nks)
-                                ptx::mma_i8_pair<true>(tmem, d_128 | (uint64_t)(a_lo + 2 * ks), d_128 | (uint64_t)(b_lo + 2 * ks), id_i8);
+                                ptx::mma_i8_pair<true>(d1, d_128 | (uint64_t)(a_lo + 2 * ks), d_128 | (uint64_t)(b_lo + 2 * ks), id_i8);
                         ptx::mma_commit_pair(bar_empty + 8 * st);
                     }
                     if (++st == kStages) { st = 0; ph ^= 1u; }
@@ -749,6 +767,11 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                 if (ok && p.a) {
                     if (!waited) { ptx::grid_dep_wait(); waited = true; }
                     const int chunks = adapters_of_tile(mt) * per_adapter;
+                    // the one accumulator of the adapters: the unit before this one has been read
+                    if (chunks && q.depth == 2 && !q.d2_step && done) {
+                        if (!wait_read(buf ^ 1u, (done + 1u) >> 1)) { ok = false; break; }
+                        ptx::tc_fence_after_sync();
+                    }
                     for (int c = 0, part = 0; c < chunks; ++c) {
                         if (!wait_full()) { ok = false; break; }
                         ptx::tc_fence_after_sync();
@@ -756,7 +779,7 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                         const int left = (k2 - 64 * part) >> 4, nks = left < 4 ? left : 4;
                         if (leader) {
                             for (int ks = 0; ks < nks; ++ks)
-                                ptx::mma_f16_pair(tmem + kD2, d_128 | (uint64_t)(a_lo + 2 * ks), d_128 | (uint64_t)(b_lo + 2 * ks), id_f16,
+                                ptx::mma_f16_pair(d2, d_128 | (uint64_t)(a_lo + 2 * ks), d_128 | (uint64_t)(b_lo + 2 * ks), id_f16,
                                                   c || ks ? 1u : 0u);
                             ptx::mma_commit_pair(bar_empty + 8 * st);
                         }
@@ -764,10 +787,10 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                         if (++st == kStages) { st = 0; ph ^= 1u; }
                     }
                 }
-                if (ok && leader) ptx::mma_commit_pair(bar_tfull);
+                if (ok && leader) ptx::mma_commit_pair(bar_tfull + 8 * buf);
             }
             // the second CTA's read-outs arrive here
-            if (ok && done) tc::wait_bar_warp(bar_tempty, (done & 1u) ^ 1u, flags);
+            for (uint32_t b = 0; ok && b < (uint32_t)q.depth; ++b) ok = wait_read(b, q.depth == 2 ? (done + 1u - b) >> 1 : done);
             if (leader) ptx::mma_commit_own(bar_drain);
             const unsigned long long t0 = ptx::globaltimer();
             while (!ptx::mbar_try_wait(bar_drain, 0) && ptx::globaltimer() - t0 < tc::kWaitLimitNs) {}
@@ -780,6 +803,8 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
         // there are few, all groups fill together, a group 32 rows.
         const int f = threadIdx.x - 32 * kFill0, grp = f / (32 * kGroupWarps), ft = f % (32 * kGroupWarps);
         const int row0 = ft >> 1, half = ft & 1;
+        constexpr int kHop = 16 * kGroupWarps, kRows = 128 / kHop;          // weights: between a thread's rows, their number
+        constexpr int kPerRow = kFillWarps / 4, kPieces = 8 / kPerRow;      // adapters: threads of a row, 16-byte pieces of each
         const uint32_t full = ptx::map_to_rank(bar_full, 0);
         const int rowb = p.cin >> 2;
         const bool wide_codes = (rowb & 15) == 0;
@@ -799,12 +824,12 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
         for (long long u = pair; u < units && ok; u += pairs) {
             const int mt = (int)(u / q.n_ctiles), ct = (int)(u % q.n_ctiles);
             const int rows = width(ct) / 2, o0 = ct * q.nt + (int)rank * rows;
-            uint32_t code[4][4];
+            uint32_t code[kRows][4];
             auto fetch = [&](int c) {
                 const int k = c * 128 + half * 64;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int row = row0 + 32 * i;
+                for (int i = 0; i < kRows; ++i) {
+                    const int row = row0 + kHop * i;
                     const bool there = row < rows && o0 + row < p.cout;
                     const uint8_t *src = p.w + (size_t)(there ? o0 + row : 0) * rowb + c * 32 + half * 16;
                     if (wide_codes) {
@@ -825,7 +850,7 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                 chunks = __ldcg(list) * per_adapter;
                 held[0] = __ldcg(list + 1);         // (what lies past the number is not used)
                 held[1] = __ldcg(list + 2);
-                const long long r = (long long)mt * kTile + (int)rank * 128 + row0 + 32 * grp;
+                const long long r = (long long)mt * kTile + (int)rank * 128 + f / kPerRow;
                 mine = r < p.m ? __ldcg(p.row_adapter + r) : -1;
             };
             if (p.a && waited) look();
@@ -836,12 +861,12 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                 if (!enter(n)) { ok = false; break; }
                 uint8_t *dst = smem + (n % kStages) * kStage + kHalfStage;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (row0 + 32 * i < rows) {
+                for (int i = 0; i < kRows; ++i)
+                    if (row0 + kHop * i < rows) {
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            invalid |= (code[i][j] >> 1) & ~code[i][j] & 0x55555555u;
-                            *reinterpret_cast<uint4 *>(dst + tc::swz_offset((uint32_t)(row0 + 32 * i), (uint32_t)(half * 4 + j), 128u)) = expand_16(code[i][j]);
+                            if (mt == 0) invalid |= (code[i][j] >> 1) & ~code[i][j] & 0x55555555u;     // (every tile of rows sees the same)
+                            *reinterpret_cast<uint4 *>(dst + tc::swz_offset((uint32_t)(row0 + kHop * i), (uint32_t)(half * 4 + j), 128u)) = expand_16(code[i][j]);
                         }
                     }
                 if (c + kFillGroups < q.kc) fetch(c + kFillGroups);
@@ -850,14 +875,14 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
             seq += (uint32_t)q.kc;
             if (!ok || !p.a) continue;
             if (!waited) { ptx::grid_dep_wait(); waited = true; look(); }
-            const int row = row0 + 32 * grp;
+            const int row = f / kPerRow, first = f % kPerRow * kPieces;
             const long long r = (long long)mt * kTile + (int)rank * 128 + row;
             const bool there = row < rows && o0 + row < p.cout, wide_b = (p.rank & 7) == 0;
-            const uint32_t off0 = tc::swz_offset((uint32_t)row, (uint32_t)(half * 4), 128u);       // piece k: off0 ^ 16 k
+            const uint32_t off0 = tc::swz_offset((uint32_t)row, (uint32_t)first, 128u);       // piece k: off0 ^ 16 k
             // a chunk is announced while the next two's copies are on their way
             auto land = [&](uint32_t n) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {       // what is not finite in B counts as zero
+                for (int k = 0; k < kPieces; ++k) {       // what is not finite in B counts as zero
                     const uint32_t at = base + (n % kStages) * kStage + kHalfStage + (off0 ^ (16u * k));
                     const int4 v = ptx::lds_128(at);
                     uint32_t w[4] = {(uint32_t)v.x, (uint32_t)v.y, (uint32_t)v.z, (uint32_t)v.w};
@@ -875,13 +900,13 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
             for (int i_ad = 0, part = 0, c2 = 0; c2 < chunks; ++c2) {
                 const uint32_t n = seq + (uint32_t)c2;
                 const int a = i_ad == 0 ? held[0] : (i_ad == 1 ? held[1] : __ldcg(list + 1 + i_ad));
-                const int e0 = part * 64 + half * 32;
+                const int e0 = part * 64 + first * 8;
                 if (!enter(n)) { ok = false; break; }
                 const uint32_t dst = base + (n % kStages) * kStage;
                 const H *t16 = static_cast<const H *>(p.t16) + (size_t)(mine == a ? r : 0) * k2;
                 const H *b = static_cast<const H *>(p.b) + ((size_t)a * p.cout + (there ? o0 + row : 0)) * p.rank;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < kPieces; ++k) {
                     const int e = e0 + 8 * k, j = e - (e >= p.pitch ? p.pitch : 0) - (e >= 2 * p.pitch ? p.pitch : 0);
                     const uint32_t off = off0 ^ (16u * k);
                     const bool t_in = e < k2 && mine == a, b_in = e < k2 && there && j < p.rank;
@@ -914,7 +939,7 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
         // ---- epilogue --------------------------------------------------------------------------------------------
         // Four groups of four warps, a warp per quarter of the rows: pieces of 32 outputs, every fourth one a group's.
         const int e = warp - kEpi0, quarter = warp & 3, grp = e >> 2;
-        uint8_t *slab = smem + kOffSlab + (size_t)e * kSlab;
+        uint8_t *slab = smem + TileLayout<Y>::kOffSlab + (size_t)e * TileLayout<Y>::kSlab;
         const uint32_t slab_addr = ptx::smem_u32(slab);
         const uint32_t t_lane = tmem + ((uint32_t)(quarter * 32) << 16);
         const uint32_t tempty = ptx::map_to_rank(bar_tempty, 0);
@@ -937,12 +962,14 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                     if (with) ad = (p.scale ? __ldg(p.scale + a) : 1.0f) * fac * __ldcg(p.power + r);
                 }
             }
-            if (!tc::wait_bar<true>(bar_tfull, done & 1u, flags)) break;
+            const uint32_t buf = q.depth == 2 ? done & 1u : 0u, use = q.depth == 2 ? done >> 1 : done;
+            const uint32_t d1 = t_lane + buf * (uint32_t)q.nt, d2 = t_lane + (uint32_t)(q.depth * q.nt) + buf * (uint32_t)q.d2_step;
+            if (!tc::wait_bar<true>(bar_tfull + 8 * buf, use & 1u, flags)) break;
             ptx::tc_fence_after_sync();
             auto release = [&] {
                 ptx::tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive_cluster(tempty);
+                if (lane == 0) ptx::mbar_arrive_cluster(tempty + 8 * buf);
             };
             if (grp >= pieces) release();
 #pragma unroll 1
@@ -953,8 +980,8 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
 #pragma unroll
                 for (int h = 0; h < 32; h += 16) {
                     uint32_t v[16], w[16];
-                    ptx::tmem_ld_x16(t_lane + (uint32_t)(pc * 32 + h), v);
-                    if (adapters) ptx::tmem_ld_x16(t_lane + kD2 + (uint32_t)(pc * 32 + h), w);
+                    ptx::tmem_ld_x16(d1 + (uint32_t)(pc * 32 + h), v);
+                    if (adapters) ptx::tmem_ld_x16(d2 + (uint32_t)(pc * 32 + h), w);
                     float al[16];
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {

@@ -2503,9 +2503,9 @@ static int tile_pairs(const DeviceInfo &d)
     const bool keep = d.dev >= 0 && d.dev < 64;
     int n = keep ? known[d.dev].load() : 0;
     if (n == 0) {
-        if (raise_smem_limit(proj_tiles_kernel<H, Y>, (int)kTileSmem) != cudaSuccess) return 0;
+        if (raise_smem_limit(proj_tiles_kernel<H, Y>, (int)TileLayout<Y>::kSmem) != cudaSuccess) return 0;
         cudaLaunchConfig_t cfg;
-        fill_launch_cfg(cfg, nullptr, 2 * (d.sms / 2), kTileThreads, kTileSmem, nullptr, false);
+        fill_launch_cfg(cfg, nullptr, 2 * (d.sms / 2), kTileThreads, TileLayout<Y>::kSmem, nullptr, false);
         if (cudaOccupancyMaxActiveClusters(&n, proj_tiles_kernel<H, Y>, &cfg) != cudaSuccess) {
             cudaGetLastError();
             n = 0;
@@ -2552,6 +2552,8 @@ static prom_status run_tiles(Params &p, int y_type, const DeviceInfo &d, cudaStr
     q.nt = 256;
     while (q.nt > 64 && (long long)q.n_mtiles * ((p.cout + q.nt - 1) / q.nt) < pairs) q.nt /= 2;
     q.n_ctiles = (p.cout + q.nt - 1) / q.nt;
+    q.depth = p.a && q.nt > 160 ? 1 : 2;
+    q.d2_step = q.nt <= 128 ? q.nt : 0;
     const size_t bytes = norm::type_bytes(y_type);
     q.store = norm::whole_pieces(p.y, p.y_pitch, bytes);
     CUtensorMap xmap, ymap;
@@ -2605,7 +2607,7 @@ static prom_status run_tiles(Params &p, int y_type, const DeviceInfo &d, cudaStr
     }
     q.p = p;
     const long long units = (long long)q.n_mtiles * q.n_ctiles;
-    fill_launch_cfg(cfg, attr, 2 * (int)(units < pairs ? units : pairs), kTileThreads, kTileSmem, st, true);
+    fill_launch_cfg(cfg, attr, 2 * (int)(units < pairs ? units : pairs), kTileThreads, TileLayout<Y>::kSmem, st, true);
     const cudaError_t e = cudaLaunchKernelEx(&cfg, proj_tiles_kernel<H, Y>, xmap, ymap, q);
     ++g_launches;
     return cuda_status(e);

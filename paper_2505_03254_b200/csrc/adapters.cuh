@@ -601,8 +601,8 @@ inner_tiles_kernel(const Params p)
 // operand layout on their way into shared memory (four pairs of warps take the stages in turn), so a stage takes 4 KB of
 // weights from L2 instead of 16 (a pair's SM would need 64 bytes a clock of both operands at the MMAs' rate, of the 58 that L2
 // gives it; this way it is 40).
-// 8192 rows 4096 -> 4096 with adapters of rank 64 take 142 us, of which the inner products in front take 29; without adapters 98
-// (2.8 POPS of 4.56).  Bound by the stages' rate, 0.4 us each where their MMAs take 0.3: narrower tiles with two accumulators of
+// 8192 rows 4096 -> 4096 with adapters of rank 64 take 142 us (161 in long runs, under the power cap), of which the inner
+// products in front take 29; without adapters 98 (2.8 POPS of 4.56).  Bound by the stages' rate, 0.4 us each where their MMAs take 0.3: narrower tiles with two accumulators of
 // each kind take longer (160 outputs 201 us, 128 outputs 223, when 256 took 154), and twice as many fillers on half as
 // many epilogue warps gain 2 % there and lose 10 % at 1024 -> 4096.
 // Behind the chunks of K come those of the adapters: for each adapter of the tile the rows' inner products (zero for rows of

@@ -4,7 +4,7 @@
 //     g = dy w,  xh = (x - mean) rstd,  dx = rstd (g - sum(g) / n - xh sum(g xh) / n),  dw = sum_r dy xh,  db = sum_r dy
 //     gamma = max |y|,  scale = 127 / max(gamma, 1e-5),  q = clip(round(y scale), -128, 127)      (as in actquant.cuh)
 // What all of them cannot do without is their bytes: x once (and dy), y, codes or dx once.  At 16384 x 4096 bf16 the forward
-// pass takes 53.8 us (5.0 TB/s, 76 % of the measured copy bandwidth), the backward pass 80.5 (5.0 TB/s); 8192 x 4096 bf16 to
+// pass takes 53.6 us (5.0 TB/s, 77 % of the measured copy bandwidth), the backward pass 76.5 to 80.5 (5.0 TB/s); 8192 x 4096 bf16 to
 // codes takes 42.1 us, there bound by its instructions (26 a value, half of them in 64 bits or for the exact quotient).
 //
 // Many rows, forward: a warp per row, in registers or in shared memory, the parameters in shared memory.  Otherwise, and in

@@ -630,8 +630,7 @@ struct Tiles {
     Params p;
     int kc, ksteps_last;        // chunks of 128 bytes of K; MMA steps in the last one
     int n_mtiles, n_ctiles, nt;
-    int depth;                  // the projection's accumulators, nt columns each (the adapters' behind them)
-    int d2_step;                // from one of the adapters' to the next; 0: there is one
+    int depth;                  // accumulators of each kind, nt columns each: the projection's, then the adapters'
     int store;                  // y has a tensor map
 };
 
@@ -745,7 +744,7 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                 const uint32_t shape = (((uint32_t)width(ct) >> 3) << 17) | ((256u >> 4) << 24);
                 const uint32_t id_i8 = (2u << 4) | (1u << 7) | (1u << 10) | shape, id_f16 = (1u << 4) | f16_types | shape;
                 const uint32_t buf = q.depth == 2 ? done & 1u : 0u, use = q.depth == 2 ? done >> 1 : done;
-                const uint32_t d1 = tmem + buf * (uint32_t)q.nt, d2 = tmem + (uint32_t)(q.depth * q.nt) + buf * (uint32_t)q.d2_step;
+                const uint32_t d1 = tmem + buf * (uint32_t)q.nt, d2 = d1 + (uint32_t)(q.depth * q.nt);
                 if (!wait_read(buf, use)) { ok = false; break; }
                 ptx::tc_fence_after_sync();
                 for (int c = 0; c < q.kc; ++c) {
@@ -767,11 +766,6 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                 if (ok && p.a) {
                     if (!waited) { ptx::grid_dep_wait(); waited = true; }
                     const int chunks = adapters_of_tile(mt) * per_adapter;
-                    // the one accumulator of the adapters: the unit before this one has been read
-                    if (chunks && q.depth == 2 && !q.d2_step && done) {
-                        if (!wait_read(buf ^ 1u, (done + 1u) >> 1)) { ok = false; break; }
-                        ptx::tc_fence_after_sync();
-                    }
                     for (int c = 0, part = 0; c < chunks; ++c) {
                         if (!wait_full()) { ok = false; break; }
                         ptx::tc_fence_after_sync();
@@ -963,7 +957,7 @@ proj_tiles_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constan
                 }
             }
             const uint32_t buf = q.depth == 2 ? done & 1u : 0u, use = q.depth == 2 ? done >> 1 : done;
-            const uint32_t d1 = t_lane + buf * (uint32_t)q.nt, d2 = t_lane + (uint32_t)(q.depth * q.nt) + buf * (uint32_t)q.d2_step;
+            const uint32_t d1 = t_lane + buf * (uint32_t)q.nt, d2 = d1 + (uint32_t)(q.depth * q.nt);
             if (!tc::wait_bar<true>(bar_tfull + 8 * buf, use & 1u, flags)) break;
             ptx::tc_fence_after_sync();
             auto release = [&] {

@@ -2552,8 +2552,7 @@ static prom_status run_tiles(Params &p, int y_type, const DeviceInfo &d, cudaStr
     q.nt = 256;
     while (q.nt > 64 && (long long)q.n_mtiles * ((p.cout + q.nt - 1) / q.nt) < pairs) q.nt /= 2;
     q.n_ctiles = (p.cout + q.nt - 1) / q.nt;
-    q.depth = p.a && q.nt > 160 ? 1 : 2;
-    q.d2_step = q.nt <= 128 ? q.nt : 0;
+    q.depth = p.a && q.nt > 128 ? 1 : 2;        // (of 512 columns)
     const size_t bytes = norm::type_bytes(y_type);
     q.store = norm::whole_pieces(p.y, p.y_pitch, bytes);
     CUtensorMap xmap, ymap;

@@ -280,6 +280,39 @@ def test_random_shapes():
         _check(_call(c, dtype=[torch.bfloat16, torch.float32, torch.float16][k % 3]), c, (k, batch, rows, cin, cout, n, rank))
 
 
+@pytest.mark.parametrize("batch,cin,cout", [(1000, 144, 4096), (1000, 2064, 2304), (5000, 48, 4096), (2600, 400, 1048)])
+def test_tiles_with_and_without_adapters_in_turn(batch, cin, cout):
+    """Several tiles per pair of CTAs, of widths with one and with two accumulators of the adapters: tiles of many adapters, of one
+    and of none behind each other."""
+    c = _case(batch, batch, 1, cin, cout, 30, 16, order="mixed")
+    tile = torch.arange(batch, device="cuda") // 256
+    c["which"] = torch.where(tile % 3 == 0, c["which"], torch.where(tile % 3 == 1, -1, 7)).int()
+    binding.debug_adapters(2)
+    try:
+        for out in (torch.bfloat16, torch.float32):
+            y = _call(c, dtype=out)
+            _check(y, c, (batch, cin, cout))
+            assert all(torch.equal(y, _call(c, dtype=out)) for _ in range(3))
+            c0 = {k: v for k, v in c.items() if k not in ("a", "b", "scale", "which")}
+            _check(_call(c0, dtype=out), c0, (batch, cin, cout))
+    finally:
+        binding.debug_adapters()
+
+
+@pytest.mark.parametrize("mode", [1, 2])
+@pytest.mark.parametrize("row", [0, 137, 260, 1031])
+def test_an_invalid_weight_code_in_any_tile(row, mode):
+    c = _case(6, 700, 1, 176, 1032, 2, 8)
+    c["packed"] = c["packed"].clone()
+    c["packed"][row, 43] = 0b10000000
+    binding.debug_adapters(mode)
+    try:
+        _call(c)
+    finally:
+        binding.debug_adapters()
+    assert binding.last_device_status() == binding.PROM_ERR_BAD_WEIGHT
+
+
 def test_refusals():
     c = _case(1, 12, 1, 64, 32, 2, 8)
     before = binding.launch_count()

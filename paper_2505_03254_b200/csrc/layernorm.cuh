@@ -261,13 +261,11 @@ template <class T> __device__ __forceinline__ double scaled_down(float f)
 }
 __device__ __forceinline__ double two_896() { return __hiloint2double(0x77F00000, 0); }
 
-// 1 / sqrt(v): the approximation and one step of Newton's method.
-__device__ __forceinline__ float inverse_root(float v)
-{
-    const float r = rsqrtf(v);
-    return v > 0.0f && v < 1e38f ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
-}
-__device__ __forceinline__ double inverse_root(double v) { return rsqrt(v); }
+// 1 / sqrt(v + eps), in every kernel the same correctly rounded operations.  (Means and variances are quotients for the same
+// reason: a product with the rounded 1 / n gives constant rows a mean beside their value, and a mean that lies halfway between
+// two binary32 numbers the wrong one.)
+__device__ __forceinline__ float inverse_root(float v, double eps) { return __fdiv_rn(1.0f, __fsqrt_rn(v + (float)eps)); }
+__device__ __forceinline__ float inverse_root(double v, double eps) { return (float)(1.0 / sqrt(v + eps)); }
 
 // ---- sums over the threads that share a row --------------------------------------------------------
 template <class A> __device__ __forceinline__ A warp_sum(A v)
@@ -466,7 +464,6 @@ forward_groups_kernel(const Fwd p)
         p.w.get_at<E>(c0 + i * hop, n, 1.0f, w[i]);
         p.b.get_at<E>(c0 + i * hop, n, 0.0f, b[i]);
     }
-    const Sum inv_n = (Sum)1 / (Sum)n;
     // codes of a whole piece in one store
     const bool wide_q = CODES && (reinterpret_cast<uintptr_t>(p.q) + (uint64_t)((long long)r0 * n + c0)) % E == 0 && (long long)all * n % E == 0;
 
@@ -504,7 +501,7 @@ forward_groups_kernel(const Fwd p)
                 }
         }
         Sum mean[2];
-        spread_2(group_sum_2(s[0], s[1], red_mean, g, p.group) * inv_n, mean);
+        spread_2(group_sum_2(s[0], s[1], red_mean, g, p.group) / (Sum)n, mean);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             s[k] = 0;
@@ -522,7 +519,7 @@ forward_groups_kernel(const Fwd p)
                 }
             }
         }
-        const float rstd_half = (float)inverse_root(group_sum_2(s[0], s[1], red_var, g, p.group) * inv_n + (Sum)p.eps);
+        const float rstd_half = inverse_root(group_sum_2(s[0], s[1], red_var, g, p.group) / (Sum)n, p.eps);
         float mu[2] = {(float)mean[0], (float)mean[1]}, rstd[2];
         spread_2(rstd_half, rstd);
         if constexpr (!CODES) {
@@ -611,7 +608,6 @@ forward_short_kernel(const Fwd p)
     float *sw = short_params, *sb = short_params + n;
     ptx::grid_dep_wait();
     ptx::grid_dep_launch();
-    const Sum inv_n = (Sum)1 / (Sum)n;
     Piece<T, E> next[V];
     auto load = [&](long long r) {
         const T *row = static_cast<const T *>(p.x) + r * p.x_pitch;
@@ -639,7 +635,7 @@ forward_short_kernel(const Fwd p)
                 else t = t + v[i].two(e);
             }
         if constexpr (!CODES) s = t.x + t.y;
-        const Sum mean = warp_sum(s) * inv_n;
+        const Sum mean = warp_sum(s) / (Sum)n;
         s = 0;
         t = both(0.0f);
 #pragma unroll
@@ -658,7 +654,7 @@ forward_short_kernel(const Fwd p)
                 }
             }
         if constexpr (!CODES) s = t.x + t.y;
-        float mu = (float)mean, rstd = (float)inverse_root(warp_sum(s) * inv_n + (Sum)p.eps);
+        float mu = (float)mean, rstd = inverse_root(warp_sum(s) / (Sum)n, p.eps);
         if constexpr (!CODES) {
             T *out = static_cast<T *>(p.y) + r * p.y_pitch;
 #pragma unroll
@@ -739,7 +735,6 @@ forward_warps_kernel(const Fwd p)
     stage_parameters<E>(p, sw, sb);
     __syncthreads();
     auto parameters = [&](int piece, float (&w)[E], float (&b)[E]) { parameters_of<E>(sw, sb, pieces, piece, w, b); };
-    const Sum inv_n = (Sum)1 / (Sum)n;
     uint32_t phase = 0;
 #pragma unroll 1
     for (; r < m; r += warps, phase ^= 1u) {
@@ -771,13 +766,13 @@ forward_warps_kernel(const Fwd p)
             }
         }
         if constexpr (!CODES) s = t.x + t.y;
-        const Sum mean = warp_sum(s + s2) * inv_n;
+        const Sum mean = warp_sum(s + s2) / (Sum)n;
         // In 64 bits the squares of the values (exact there) can be summed on the same pass: what their difference to the mean's
         // square loses is seen, and where it is more than twelve bits the differences are taken after all.
         Sum var = 0;
         bool again = true;
         if constexpr (CODES) {
-            var = fma(-mean, mean, warp_sum(sq + sq2) * inv_n);
+            var = fma(-mean, mean, warp_sum(sq + sq2) / (Sum)n);
             again = !(var * 4096.0 >= mean * mean);
         }
         if (again) {
@@ -799,9 +794,9 @@ forward_warps_kernel(const Fwd p)
                 }
             }
             if constexpr (!CODES) s = t.x + t.y;
-            var = warp_sum(s + s2) * inv_n;
+            var = warp_sum(s + s2) / (Sum)n;
         }
-        float mu = (float)mean, rstd = (float)inverse_root(var + (Sum)p.eps);
+        float mu = (float)mean, rstd = inverse_root(var, p.eps);
         if constexpr (!CODES) {
             T *out = static_cast<T *>(p.y) + r * p.y_pitch;
 #pragma unroll 2
@@ -911,9 +906,7 @@ forward_kernel(const Fwd p)
             }
         }
     s = block_sum(s, red[1]);
-    float rstd;
-    if constexpr (CODES) rstd = (float)(1.0 / sqrt(s / (double)p.n + p.eps));
-    else rstd = 1.0f / sqrtf(s / (float)p.n + (float)p.eps);
+    const float rstd = inverse_root(s / (Sum)p.n, p.eps);
     const float mu = (float)mean;
     if (t == 0) {
         if (p.mean) p.mean[r] = mu;
@@ -1001,9 +994,7 @@ forward_long_kernel(const Fwd p)
         s += d * d;
     }
     s = block_sum(s, red[1]);
-    float rstd;
-    if constexpr (CODES) rstd = (float)(1.0 / sqrt(s / (double)p.n + p.eps));
-    else rstd = 1.0f / sqrtf(s / (float)p.n + (float)p.eps);
+    const float rstd = inverse_root(s / (Sum)p.n, p.eps);
     const float mu = (float)mean;
     if (threadIdx.x == 0) {
         if (p.mean) p.mean[r] = mu;

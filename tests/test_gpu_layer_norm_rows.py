@@ -1,0 +1,95 @@
+"""Layer norm where the number of rows chooses the kernel: the same rows in calls of a few rows and of thousands, every row
+compared, in the three types.  With S multiprocessors, calls of 8 S rows and more of whole 16-byte pieces take a warp per row (in
+registers up to 64 or 128 pieces, in shared memory above), rows that start anywhere take groups of threads, and few rows a block each.
+
+Tolerances are those of the formula: u = 2^-24, 256 u of a row's largest term, plus half a step of the output's type.  Codes
+and their statistics are compared bit for bit with the definition: sums in binary64 (exact here for the mean of 16-bit
+values), a division, one rounding to binary32."""
+import pytest
+import torch
+
+from paper_2505_03254_b200 import binding, build
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+EPS = 1e-5
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    build.build()
+    binding.last_device_status()
+    yield
+    assert binding.last_device_status() == binding.PROM_OK
+
+
+def _many():
+    """Rows from which on a warp takes each, and a few more."""
+    return 8 * torch.cuda.get_device_properties(0).multi_processor_count + 37
+
+
+def _statistics(x, eps=EPS):
+    xd = x.double()
+    n = torch.full((len(x), 1), float(x.shape[1]), dtype=torch.float64, device="cuda")     # (by a number, a product with its inverse)
+    mean = xd.sum(1, keepdim=True) / n
+    var = torch.square(xd - mean).sum(1, keepdim=True) / n
+    return mean, 1 / torch.sqrt(var + eps)
+
+
+def _codes(x, w, b, eps=EPS):
+    """(q, gamma, scale, mean, rstd) of the definition."""
+    mean, rstd = (t.float() for t in _statistics(x, eps))
+    y = (x.float() - mean) * rstd
+    y = y * w.float()
+    y = y + b.float()
+    gamma = y.abs().amax(1)
+    scale = torch.full_like(gamma, 127.0) / gamma.clamp(min=1e-5)
+    return torch.round(y * scale[:, None]).clamp(-128, 127).to(torch.int8), gamma, scale, mean[:, 0], rstd[:, 0]
+
+
+def _run_codes(x, w, b, eps=EPS):
+    stats = tuple(torch.empty(x.shape[0], device="cuda") for _ in range(2))
+    return (*binding.layer_norm_i8(x, w, b, eps, stats=stats), *stats)
+
+
+def _rows_apart(x, by):
+    """The same values with `by` more between the rows' starts."""
+    m, n = x.shape
+    buf = torch.full((m, n + by), 7.0, dtype=x.dtype, device="cuda")
+    buf[:, :n] = x
+    return buf[:, :n]
+
+
+def _halfway_rows(n, dtype):
+    """Rows whose mean is 1.5 + (2 i + 1) 2^-24, halfway between two binary32 numbers: 1.5, and (2 i + 1) n 2^-24 in two values."""
+    rows = torch.full((200, n), 1.5, dtype=torch.float64)
+    for i in range(200):
+        d = (2 * i + 1) * n
+        low = (n & -n) << 8             # d in pieces of eight bits at most
+        rows[i, 3], rows[i, n // 2], rows[i, n - 1] = 4.5, d % low * U, d // low * low * U
+    got = rows.to(dtype)
+    assert torch.equal(got.double(), rows)
+    return got.cuda()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [328, 392, 1568, 2624])
+def test_statistics_do_not_depend_on_the_number_of_rows(n, dtype):
+    """A division by n and no product with its rounded inverse: a constant row's mean is its value, and a mean halfway between two
+    binary32 numbers is rounded to the even one, however many rows there are and wherever they start."""
+    g = torch.Generator().manual_seed(n)
+    whole = torch.randint(1, 257, (200, 1), generator=g).double().expand(200, n).to(dtype).cuda()
+    x = torch.cat([_halfway_rows(n, dtype), whole, torch.randn((200, n), generator=g).to(dtype).cuda()])
+    x = x.repeat(-(-_many() // len(x)), 1)
+    w, b = (1 + 0.2 * torch.randn(n, generator=g)).cuda(), (0.2 * torch.randn(n, generator=g)).cuda()
+    want = _codes(x, w, b)
+    for kind, rows in {"apart": _rows_apart(x, 1), "dense": x}.items():
+        for m in (4, 403, len(x)):
+            for name, p, q in zip(("codes", "gamma", "scale", "mean", "rstd"), _run_codes(rows[:m], w, b), want):
+                bad = (p != q[:m]).view(m, -1).any(1).nonzero()[:, 0].tolist()
+                assert not bad, (kind, m, name, len(bad), bad[:5])
+            y, mean, _ = binding.layer_norm(rows[:m], None, None, EPS)
+            flat = torch.arange(m, device="cuda") % 600 // 200 == 1
+            assert torch.equal(mean[flat], rows[:m][flat][:, 0].float()) and not bool(y[flat].any()), (kind, m)

@@ -264,7 +264,10 @@ prom_status prom_layer_norm(const void *x_dev, prom_type type, int64_t m, int n,
  *     gamma = max |y|,  scale = 127 / max(gamma, 1e-5),  q = clip(round(y * scale), -128, 127)     ties to even
  * so that q and gamma are what a projection takes (rows_per_sample 1).  Mean and variance are taken in binary64, mean
  * and rstd rounded once to binary32, and x - mean, * rstd, * weight, + bias, the quotient and the last product are
- * single binary32 operations in this order: the codes do not depend on how the work is split.
+ * single binary32 operations in this order.  How the work is split decides the order of the binary64 sums alone: it moves
+ * them by a few 2^-52, and so shows only in a row (some in 10^8) whose mean or rstd lies that near to halfway between two
+ * binary32 numbers, which may then be either of them.  (Sums of 16-bit values of like size are exact, and their mean
+ * never depends on it.)
  *   q_dev  [m][n] int8;  gamma_dev, scale_dev  [m] float32;  mean_dev, rstd_dev  [m] float32 or NULL (for
  *          prom_layer_norm_backward behind a quantiser that passes gradients straight through)
  * A row with a value that is not finite has a gamma that is not finite and codes without meaning.  Everything else as

@@ -93,3 +93,18 @@ def test_statistics_do_not_depend_on_the_number_of_rows(n, dtype):
             y, mean, _ = binding.layer_norm(rows[:m], None, None, EPS)
             flat = torch.arange(m, device="cuda") % 600 // 200 == 1
             assert torch.equal(mean[flat], rows[:m][flat][:, 0].float()) and not bool(y[flat].any()), (kind, m)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_codes_of_rows_far_from_zero(dtype):
+    """Offsets of 20 to 60 times the spread: rstd is still the binary64 one rounded once (its neighbour in some rows, where the
+    variance came from the sum of squares)."""
+    m, n = 400_000, 520
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = (torch.randn((m, n), device="cuda", generator=g) + 20 + 40 * torch.rand((m, 1), device="cuda", generator=g)).to(dtype)
+    w, b = 1 + 0.2 * torch.randn(n, device="cuda", generator=g), 0.2 * torch.randn(n, device="cuda", generator=g)
+    got = _run_codes(x, w, b)
+    for lo in range(0, m, 50_000):
+        for name, p, q in zip(("codes", "gamma", "scale", "mean", "rstd"), got, _codes(x[lo:lo + 50_000], w, b)):
+            bad = (p[lo:lo + 50_000] != q).view(len(q), -1).any(1).nonzero()[:, 0].tolist()
+            assert not bad, (name, lo, len(bad), bad[:5])

@@ -270,8 +270,9 @@ prom_status prom_layer_norm(const void *x_dev, prom_type type, int64_t m, int n,
  * never depends on it.)
  *   q_dev  [m][n] int8;  gamma_dev, scale_dev  [m] float32;  mean_dev, rstd_dev  [m] float32 or NULL (for
  *          prom_layer_norm_backward behind a quantiser that passes gradients straight through)
- * A row with a value that is not finite has a gamma that is not finite and codes without meaning.  Everything else as
- * in prom_layer_norm. */
+ * A row with a value that is not finite has what the formula gives: an infinite or NaN mean, and NaN as rstd, gamma and
+ * scale.  With a parameter that is not finite, or a y beyond binary32, the statistics are x's and gamma is infinite or NaN.
+ * Codes behind a gamma that is not finite are without meaning.  Everything else as in prom_layer_norm. */
 prom_status prom_layer_norm_i8(const void *x_dev, prom_type type, int64_t m, int n, int64_t x_pitch,
                                const void *weight_dev, const void *bias_dev, prom_type param_type, double eps,
                                int8_t *q_dev, float *gamma_dev, float *scale_dev, float *mean_dev, float *rstd_dev,

@@ -313,6 +313,21 @@ __device__ __forceinline__ float affine_exact(float x, float mean, float rstd, f
     return __fadd_rn(__fmul_rn(__fmul_rn(__fsub_rn(x, mean), rstd), w), b);
 }
 
+// The maximum of a row to codes is not finite: because its values are not, or because a parameter is not or y overflows.  The
+// sum of what is not finite in it over one thread's part, 0 where all is finite.  (The statistics' sums take such bits for
+// a number's; the formula's mean is this sum over all threads, and NaN is what the rest of the row becomes.)
+template <class T> __device__ __forceinline__ float sum_not_finite(const Fwd &p, long long r, int first, int hop)
+{
+    const T *row = static_cast<const T *>(p.x) + r * p.x_pitch;
+    float s = 0.0f;
+    for (int c = first; c < p.n; c += hop) {
+        const float f = to_float(row[c]);
+        s += fabsf(f) <= 3.402823466e38f ? 0.0f : f;
+    }
+    return s;
+}
+__device__ __forceinline__ bool not_finite(float v) { return !(fabsf(v) <= 3.402823466e38f); }
+
 // E codes of neighbouring columns in one store (E is 1, 4 or 8; the row's codes are E-aligned).
 template <int E> __device__ __forceinline__ void store_codes(int8_t *q, const float (&y)[E], float scale)
 {
@@ -554,8 +569,19 @@ forward_groups_kernel(const Fwd p)
                                 top[k] = max_nan(top[k], fabsf(affine_exact(v[k][i].get(e), mu[k], rstd[k], w[i][e], b[i][e])));
                     }
             }
-            const float top_half = group_max_2(top[0], top[1], red_max, g, p.group);
+            float top_half = group_max_2(top[0], top[1], red_max, g, p.group);
             spread_2(top_half, top);
+            if (not_finite(top[0]) || not_finite(top[1])) {         // (the same for all of the group)
+                float odd[2];
+                odd[0] = sum_not_finite<T>(p, r, t, p.group);
+                odd[1] = two ? sum_not_finite<T>(p, r + all, t, p.group) : 0.0f;
+                Sum all_odd[2];
+                spread_2(group_sum_2((Sum)odd[0], (Sum)odd[1], red_var, g, p.group), all_odd);     // (read before the barrier behind the maximum)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (all_odd[k] != (Sum)0) { mu[k] = (float)all_odd[k]; rstd[k] = top[k] = __int_as_float(0x7FC00000); }
+                top_half = (threadIdx.x & 16) ? top[1] : top[0];
+            }
             spread_2(actq::scale_of(top_half, 1e-5f), scale);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -577,8 +603,6 @@ forward_groups_kernel(const Fwd p)
                                 if (inside(i, e)) out[e] = actq::quantise_one(f[e], scale[k]);
                         }
                     }
-                // (a value that is not finite shows in the maximum only: the sums took its bits for a number's)
-                if (!(top[k] <= 3.402823466e38f)) mu[k] = rstd[k] = __int_as_float(0x7FC00000);
             }
         }
         if (t == 0) {
@@ -686,12 +710,15 @@ forward_short_kernel(const Fwd p)
                     }
                 }
             top = warp_max(top);
+            if (not_finite(top)) {
+                const float odd = warp_sum(sum_not_finite<T>(p, r, lane, 32));
+                if (odd != 0.0f) { mu = odd; rstd = top = __int_as_float(0x7FC00000); }
+            }
             const float sc = actq::scale_of(top, 1e-5f);
             if (lane == 0) { p.gamma[r] = top; p.scale[r] = sc; }
 #pragma unroll
             for (int i = 0; i < V; ++i)
                 if (lane + 32 * i < pieces) store_codes<E>(p.q + r * n + (lane + 32 * i) * E, y[i], sc);
-            if (!(top <= 3.402823466e38f)) mu = rstd = __int_as_float(0x7FC00000);      // (as in the next kernel)
         }
         if (lane == 0) {
             if (p.mean) p.mean[r] = mu;
@@ -826,6 +853,10 @@ forward_warps_kernel(const Fwd p)
                 for (int e = 0; e < E; ++e) top = max_nan(top, fabsf(affine_exact(v.get(e), mu, rstd, w[e], b[e])));
             }
             top = warp_max(top);
+            if (not_finite(top)) {
+                const float odd = warp_sum(sum_not_finite<T>(p, r, lane, 32));
+                if (odd != 0.0f) { mu = odd; rstd = top = __int_as_float(0x7FC00000); }
+            }
             const float sc = actq::scale_of(top, 1e-5f);
             if (lane == 0) { p.gamma[r] = top; p.scale[r] = sc; }
             int8_t *out = p.q + r * n;
@@ -838,8 +869,6 @@ forward_warps_kernel(const Fwd p)
                 for (int e = 0; e < E; ++e) w[e] = affine_exact(v.get(e), mu, rstd, w[e], b[e]);
                 store_codes<E>(out + i * E, w, sc);
             }
-            // (a value that is not finite shows in the maximum only: the sums took its bits for a number's)
-            if (!(top <= 3.402823466e38f)) mu = rstd = __int_as_float(0x7FC00000);
         }
         if (lane == 0) {
             if (p.mean) p.mean[r] = mu;
@@ -878,20 +907,13 @@ forward_kernel(const Fwd p)
         if (t + i * threads < pieces) v[i].load(row + (size_t)(t + i * threads) * E);
 
     Sum s = 0;
-    float odd = 0.0f;                   // NaN once a value is not finite
 #pragma unroll
     for (int i = 0; i < V; ++i)
 #pragma unroll
         for (int e = 0; e < E; ++e) {   // (what lies past the row is zero)
-            const float f = v[i].get(e);
-            if constexpr (CODES) {
-                s = fma(scaled_down<T>(f), two_896(), s);
-                odd = fmaf(f, 0.0f, odd);
-            } else {
-                s += f;
-            }
+            if constexpr (CODES) s = fma(scaled_down<T>(v[i].get(e)), two_896(), s);
+            else s += v[i].get(e);
         }
-    if constexpr (CODES) s += (double)odd;
     s = block_sum(s, red[0]);
     const Sum mean = s / (Sum)p.n;
     s = 0;
@@ -908,12 +930,7 @@ forward_kernel(const Fwd p)
             }
         }
     s = block_sum(s, red[1]);
-    const float rstd = inverse_root(s / (Sum)p.n, p.eps);
-    const float mu = (float)mean;
-    if (t == 0) {
-        if (p.mean) p.mean[r] = mu;
-        if (p.rstd) p.rstd[r] = rstd;
-    }
+    float rstd = inverse_root(s / (Sum)p.n, p.eps), mu = (float)mean;
     if constexpr (!CODES) {
         T *out = static_cast<T *>(p.y) + r * p.y_pitch;
 #pragma unroll
@@ -952,6 +969,10 @@ forward_kernel(const Fwd p)
             }
         }
         top = block_max(top, red_max);
+        if (not_finite(top)) {
+            const Sum odd = block_sum((Sum)sum_not_finite<T>(p, r, t, threads), red[0]);       // (read before the last two barriers)
+            if (odd != (Sum)0) { mu = (float)odd; rstd = top = __int_as_float(0x7FC00000); }
+        }
         const float sc = actq::scale_of(top, 1e-5f);
         if (t == 0) { p.gamma[r] = top; p.scale[r] = sc; }
         int8_t *out = p.q + r * p.n;
@@ -972,6 +993,10 @@ forward_kernel(const Fwd p)
                 }
             }
         }
+    }
+    if (t == 0) {
+        if (p.mean) p.mean[r] = mu;
+        if (p.rstd) p.rstd[r] = rstd;
     }
 }
 

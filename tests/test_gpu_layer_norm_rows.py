@@ -108,3 +108,45 @@ def test_codes_of_rows_far_from_zero(dtype):
         for name, p, q in zip(("codes", "gamma", "scale", "mean", "rstd"), got, _codes(x[lo:lo + 50_000], w, b)):
             bad = (p[lo:lo + 50_000] != q).view(len(q), -1).any(1).nonzero()[:, 0].tolist()
             assert not bad, (name, lo, len(bad), bad[:5])
+
+
+def _same(p, q):
+    return bool(((p == q) | (torch.isnan(p) & torch.isnan(q))).all())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [128, 250, 264, 768, 2048, 4100, 16401])
+def test_codes_of_values_that_are_not_finite(n, dtype):
+    """The statistics are the formula's, whichever kernel takes the row: an infinity in x shows in the mean and makes the rest NaN,
+    one in a parameter leaves mean and rstd alone."""
+    many = _many()
+    m = many if n < 16401 else 40
+    x = torch.randn((m, n), device="cuda", generator=torch.Generator(device="cuda").manual_seed(n)).to(dtype)
+    inf = float("inf")
+    for at in (0, m // 2, m - 9):
+        x[at, 7], x[at + 1, n - 1], x[at + 2, 0] = inf, -inf, float("nan")
+        x[at + 3, 1], x[at + 3, n // 2] = inf, -inf
+    bad = torch.tensor([r + k for r in (0, m // 2, m - 9) for k in range(4)], device="cuda")
+    good = torch.ones(m, dtype=torch.bool, device="cuda")
+    good[bad] = False
+    w, b = torch.ones(n, device="cuda"), torch.zeros(n, device="cuda")
+    want = _codes(x, w, b)
+    for rows in (x, _rows_apart(x, 3), x[:5], _rows_apart(x[:5], 1)):
+        q, gamma, scale, mean, rstd = _run_codes(rows, w, b)
+        assert _same(mean, want[3][:len(rows)]) and _same(rstd, want[4][:len(rows)])
+        assert _same(gamma, want[1][:len(rows)]) and _same(scale, want[2][:len(rows)])
+        assert torch.equal(q[good[:len(rows)]], want[0][:len(rows)][good[:len(rows)]])
+        assert bool(torch.isnan(gamma[bad[bad < len(rows)]]).all()) and bool(torch.isinf(mean[:2]).all())
+    # parameters that are not finite, and values beyond binary32 behind finite ones
+    for key, value in (("b", inf), ("w", float("nan")), ("w", 3e38)):
+        w2, b2 = w.clone(), b.clone()
+        (w2 if key == "w" else b2)[n - 2] = value
+        x2 = x.clone()
+        x2[bad] = 1.0
+        x2[:, n - 2] = 50.0
+        want = _codes(x2, w2, b2)
+        for rows in (x2, _rows_apart(x2, 3), x2[:5], _rows_apart(x2[:5], 1)):
+            q, gamma, scale, mean, rstd = _run_codes(rows, w2, b2)
+            assert bool(torch.isfinite(mean).all()) and bool(torch.isfinite(rstd).all())
+            assert _same(mean, want[3][:len(rows)]) and _same(rstd, want[4][:len(rows)])
+            assert _same(gamma, want[1][:len(rows)]) and not bool(torch.isfinite(gamma).any())

@@ -129,19 +129,27 @@ template <class T, int E> struct Piece {
     // From here on the values are converted again instead of being kept as floats, twice the registers of 16-bit ones.
     __device__ __forceinline__ void again() { asm volatile("" : "+r"(raw.x), "+r"(raw.y), "+r"(raw.z), "+r"(raw.w)); }
 };
-// The piece of columns c .. c + E - 1 of a row of n, of which some may lie outside it.
-template <class T, int E> __device__ __forceinline__ void load_at(Piece<T, E> &v, const T *row, int c, int n)
+// The piece of columns c .. c + E - 1 of a row of n, of which some may lie outside it: zeros, or with NEAREST the row's first or
+// last value (for x in the backward pass: zero less a large mean, times rstd, may be infinite, and a zero gradient times that
+// NaN).
+template <bool NEAREST = false, class T, int E> __device__ __forceinline__ void load_at(Piece<T, E> &v, const T *row, int c, int n)
 {
     if (c >= 0 && c + E <= n) {
         v.load(row + c);
     } else {
+        auto bits = [&](int at) -> uint32_t {
+            if constexpr (sizeof(T) == 4) return __float_as_uint((float)row[at]);
+            else return reinterpret_cast<const uint16_t *>(row)[at];
+        };
+        const uint32_t beside = NEAREST ? bits(c < 0 ? 0 : n - 1) : 0u;
         uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (c + e >= 0 && c + e < n) {
-                if constexpr (sizeof(T) == 4) w[e] = __float_as_uint((float)row[c + e]);
-                else w[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[c + e] << (16 * (e & 1));
-            }
+        for (int e = 0; e < E; ++e) {
+            uint32_t one = beside;
+            if (c + e >= 0 && c + e < n) one = bits(c + e);
+            if constexpr (sizeof(T) == 4) w[e] = one;
+            else w[e / 2] |= one << (16 * (e & 1));
+        }
         v.raw = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
@@ -488,7 +496,7 @@ forward_groups_kernel(const Fwd p)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             to[i].raw = make_uint4(0u, 0u, 0u, 0u);
-            if (r < m && some(i)) load_at<T, E>(to[i], row, c0 + i * hop, n);
+            if (r < m && some(i)) load_at(to[i], row, c0 + i * hop, n);
         }
     };
     auto later = [&](int r, int k) { return (long long)r + (long long)k * all < m ? r + k * all : m; };
@@ -1137,8 +1145,8 @@ backward_kernel(const Bwd p)
             if (r < m && in_row(i)) {
                 const T *xr = x + r * p.x_pitch, *dr = dy + r * p.dy_pitch;
                 if constexpr (kShift) {
-                    load_at<T, E>(next_x[i], xr, c0 + i * hop, n);
-                    load_at<T, E>(next_d[i], dr, c0 + i * hop, n);
+                    load_at<true>(next_x[i], xr, c0 + i * hop, n);
+                    load_at(next_d[i], dr, c0 + i * hop, n);
                 } else {
                     next_x[i].load(xr + c0 + i * hop);
                     next_d[i].load(dr + c0 + i * hop);

@@ -150,3 +150,18 @@ def test_codes_of_values_that_are_not_finite(n, dtype):
             assert bool(torch.isfinite(mean).all()) and bool(torch.isfinite(rstd).all())
             assert _same(mean, want[3][:len(rows)]) and _same(rstd, want[4][:len(rows)])
             assert _same(gamma, want[1][:len(rows)]) and not bool(torch.isfinite(gamma).any())
+
+
+@pytest.mark.parametrize("n", [129, 1283])
+def test_backward_of_constant_rows_of_large_values(n):
+    """xh is zero in all of the row and only there: what stands beside a row in its last piece of memory (mean rstd is 6e38) takes
+    no part in its sums."""
+    m = 40
+    x = torch.full((m, n), 2e36, device="cuda")
+    dy = torch.randn((m, n), device="cuda", generator=torch.Generator(device="cuda").manual_seed(n))
+    mean, rstd = torch.full((m,), 2e36, device="cuda"), torch.full((m,), 316.25, device="cuda")
+    dx, dw, db = binding.layer_norm_backward(dy, x, None, mean, rstd)
+    g = dy.double()
+    want = 316.25 * (g - g.mean(1, keepdim=True))
+    assert bool(((dx.double() - want).abs() <= 316.25 * 256 * U * g.abs().amax(1, keepdim=True)).all())
+    assert not bool(dw.any()) and bool(((db.double() - g.sum(0)).abs() <= 256 * U * g.abs().sum(0)).all())

@@ -314,7 +314,8 @@ typedef struct {
  *     y[r][o] = (sum_k x[r][k] * W-hat[o][k]) * alpha[o] * f
  *             + scale[a] * f * sum_j B[a][o][j] * (sum_k A[a][j][k] * x[r][k])          (a >= 0)
  * The first sum is exact, the others and the factors are taken in binary32 (the inner products, where the tensor cores
- * take them as 16-bit values, as a sum of two such values, or of three for float32 outputs), y is rounded once.
+ * take them as 16-bit values, as a sum of three such values, or of two float16 ones, 22 bits, for 16-bit outputs), y is
+ * rounded once.
  *   x_dev        [batch * rows_per_sample][cin] int8, 16-byte aligned; gamma_x_dev [batch] float32 (both as
  *                prom_layer_norm_i8 and prom_quantize_act_absmax give them: one sample a token, or an image)
  *   w_packed_dev, alpha_dev   as for prom_pw_conv_i8_dyn

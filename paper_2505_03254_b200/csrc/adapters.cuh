@@ -606,7 +606,7 @@ inner_tiles_kernel(const Params p)
 // each kind take longer (160 outputs 201 us, 128 outputs 223, when 256 took 154), and twice as many fillers on half as
 // many epilogue warps gain 2 % there and lose 10 % at 1024 -> 4096.
 // Behind the chunks of K come those of the adapters: for each adapter of the tile the rows' inner products (zero for rows of
-// other adapters), as sums of 16-bit values (two, or three for binary32 outputs) side by side along K, against B
+// other adapters), as sums of 16-bit values (three, or two float16 ones for 16-bit outputs) side by side along K, against B
 // repeated as often.
 constexpr int kFillGroups = 4, kGroupWarps = 2, kFillWarps = kFillGroups * kGroupWarps;
 constexpr int kEpiGroups = 4, kEpiWarps = 4 * kEpiGroups;

@@ -2478,7 +2478,9 @@ static prom_status run_rows(Params &p, const DeviceInfo &d, cudaStream_t st)
 // 14.0 / 16.2, 512 rows 22.1 / 15.2; at 4096 -> 4096: 64 rows 14.2 / 23.5, 128 rows 25.6 / 24.2; without adapters 64 rows
 // 9.7 / 13.4, 96 rows 14.8 / 13.6.  Inner products cost the first per row and rank, the tiled ones per adapter that a tile
 // of rows may have (416 -> 2576, 181 rows, 16 adapters: 13.7 / 23.5; 80 -> 40, 672 rows, one adapter of rank 32:
-// 13.3 / 10.6).
+// 13.3 / 10.6).  Higher ranks, which the fit has not seen: 1024 -> 1024 and 4096 -> 4096, 64 to 512 rows, two and eight
+// adapters of rank 64, 128 and 256: its choice is the faster one or within 11 % of it (256 rows 1024 -> 1024, two of rank 64:
+// 22.0 / 19.8).
 static bool rows_faster(const Params &p, int pairs)
 {
     if (p.m > 65535ll * 32) return false;
@@ -2585,7 +2587,11 @@ static prom_status run_tiles(Params &p, int y_type, const DeviceInfo &d, cudaStr
     cudaLaunchAttribute attr[1];
     if (p.a) {
         p.pitch = pitch_of(p.rank);
-        p.terms = y_type == PROM_TYPE_F32 ? 3 : 2;
+        // What a row's inner products keep does not depend on how many rows the call has: three bfloat16 values are the 24 bits of
+        // the kernels for few rows, three float16 ones more, and two float16 ones, which 16-bit outputs take, 22 bits.  (Two bfloat16
+        // values, 16 bits, showed where an adapter takes the projection away; they are 2 % faster at 8192 rows 4096 -> 4096,
+        // rank 64, and at most 16 %, at 512 rows with eight adapters a tile.)
+        p.terms = y_type == PROM_TYPE_F32 || std::is_same<H, __nv_bfloat16>::value ? 3 : 2;
         uint8_t *ws = reinterpret_cast<uint8_t *>(p.t);
         p.t16 = ws;
         p.power = reinterpret_cast<float *>(ws + t16_bytes(p.m, p.rank));

@@ -217,6 +217,11 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar)
 {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
+// n arrivals on a barrier of either CTA, for operands that the thread's warp has written into the shared memory of its own CTA.
+// The caller has passed fence_proxy_async_smem in every writing thread and a __syncwarp: from there on the tensor core and the
+// copies of this SM see them, and those are the only ones that read them (an MMA of a pair takes each CTA's operands from that
+// CTA's SM).  What crosses to the other CTA is the signal to issue; no thread there reads the memory, and it hands
+// over none that one would.
 __device__ __forceinline__ void mbar_arrive_cluster_n(uint32_t cluster_bar, uint32_t n)
 {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0], %1;" ::"r"(cluster_bar), "r"(n) : "memory");

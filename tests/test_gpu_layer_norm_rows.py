@@ -165,3 +165,127 @@ def test_backward_of_constant_rows_of_large_values(n):
     want = 316.25 * (g - g.mean(1, keepdim=True))
     assert bool(((dx.double() - want).abs() <= 316.25 * 256 * U * g.abs().amax(1, keepdim=True)).all())
     assert not bool(dw.any()) and bool(((db.double() - g.sum(0)).abs() <= 256 * U * g.abs().sum(0)).all())
+
+
+def _near(got, want, slack, what):
+    """|got - want| <= slack + half a step of got's type."""
+    err = (got.double() - want).abs()
+    info = torch.finfo(got.dtype)
+    lim = slack + info.eps / 2 * 1.001 * want.abs() + info.tiny * info.eps
+    bad = ~(err <= lim)
+    assert not bool(bad.any()), (what, int(bad.sum()), [int(v) for v in bad.nonzero()[0]], float((err / lim).max()))
+
+
+def _rows(seed, m, n, dtype, pitch=0):
+    """Rows of a residual stream: scales and offsets of their own, every 16th one far from zero for its spread."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn((m, n), device="cuda", generator=g) * torch.exp(torch.randn((m, 1), device="cuda", generator=g))
+    x += 0.3 * torch.randn((m, 1), device="cuda", generator=g)
+    x[::16] += 100 * x[::16].std(1, keepdim=True) if n > 1 else 0.0
+    x = x.to(dtype)
+    w = 1 + 0.2 * torch.randn(n, device="cuda", generator=g)
+    b = 0.2 * torch.randn(n, device="cuda", generator=g)
+    return (_rows_apart(x, pitch) if pitch else x), w, b
+
+
+# widths on both sides of where the kernels for many rows change, in 16-byte pieces: 32, 64 and 128 (registers), 512 and, for
+# codes, 4096 values (shared memory); several rows of a warp in turn
+WIDTHS = [8, 24, 96, 128, 132, 192, 256, 260, 264, 384, 512, 520, 768, 1024, 1032, 2048, 2056, 4096, 4104]
+
+
+def _count(n):
+    """Rows: three rounds of the warps that an SM holds at most, or enough for the kernels of many rows where that is much."""
+    return 3 * 32 * torch.cuda.get_device_properties(0).multi_processor_count + 11 if n <= 1032 else _many() if n > 4096 else 8999
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", WIDTHS)
+def test_forward_of_many_rows(n, dtype):
+    m = _count(n)
+    x, w, b = _rows(n, m, n, dtype)
+    mu, rs = _statistics(x)
+    top = (x.double().abs().amax(1, keepdim=True) + mu.abs()) * rs + 1
+    slack = 256 * U * top * (w.double().abs() + 1)
+    want = (x.double() - mu) * rs * w.double() + b.double()
+    y, mean, rstd = binding.layer_norm(x, w, b, EPS)
+    _near(y, want, slack, "y")
+    _near(mean, mu[:, 0], 256 * U * x.double().abs().amax(1), "mean")
+    _near(rstd, rs[:, 0], 256 * U * top[:, 0] * rs[:, 0], "rstd")
+    # rows of a wider buffer, and in place: the same kernel, the same bits
+    apart = _rows_apart(x, 16)
+    assert torch.equal(binding.layer_norm(apart, w, b, EPS, out=(_rows_apart(x, 24), None, None))[0], y)
+    assert torch.equal(binding.layer_norm(apart, w, b, EPS, out=(apart, None, None))[0], y)
+    assert bool((torch.as_strided(apart, (m, 16), (n + 16, 1), n)[: m - 1] == 7.0).all())
+    own = x.clone()
+    binding.layer_norm(own, w, b, EPS, out=(own, None, None))
+    assert torch.equal(own, y)
+    kept = dtype if dtype != torch.float32 else torch.bfloat16          # parameters of a 16-bit type
+    w2, b2 = w.to(kept), b.to(kept)
+    _near(binding.layer_norm(x, w2, b2, EPS)[0], (x.double() - mu) * rs * w2.double() + b2.double(), slack * 1.01, "y")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", WIDTHS)
+def test_codes_of_many_rows(n, dtype):
+    m = _count(n)
+    x, w, b = _rows(n + 1, m, n, dtype)
+    want = _codes(x, w, b)
+    for rows in (x, _rows_apart(x, 16), _rows_apart(x, 1)):
+        for name, p, q in zip(("codes", "gamma", "scale", "mean", "rstd"), _run_codes(rows, w, b), want):
+            bad = (p != q).view(m, -1).any(1).nonzero()[:, 0].tolist()
+            assert not bad, (name, len(bad), bad[:5])
+
+
+# rows of a group of threads that go round its ring of copies several times; in 16-byte pieces 65 to 1024 (two a thread) and up
+# to 2048 (four)
+RINGS = [(9001, 520), (9001, 1024), (7001, 1536), (4001, 2048), (3001, 4096), (1501, 8192), (1201, 12288), (901, 16384)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n", RINGS)
+def test_backward_of_many_rows(m, n, dtype):
+    if dtype == torch.float32:
+        n //= 2
+    x, w, _ = _rows(n + 2, m, n, dtype)
+    dy = torch.randn((m, n), device="cuda", generator=torch.Generator(device="cuda").manual_seed(n)).to(dtype)
+    mean, rstd = (t[:, 0].float() for t in _statistics(x))
+    dx, dw, db = binding.layer_norm_backward(dy, x, w, mean, rstd)
+    rd = rstd.double()[:, None]
+    xh = (x.double() - mean.double()[:, None]) * rd
+    gd = dy.double() * w.double()
+    want = rd * (gd - gd.mean(1, keepdim=True) - xh * (gd * xh).mean(1, keepdim=True))
+    top = ((x.double().abs() + mean.double().abs()[:, None]) * rd).amax(1, keepdim=True) + 1
+    _near(dx, want, 256 * U * rd * gd.abs().amax(1, keepdim=True) * top * top, "dx")
+    # a thread adds up to m / 148 rows behind each other, of sizes that add up to a 148th of the column's
+    long = max(256.0, m / 148.0)
+    _near(dw, (dy.double() * xh).sum(0), long * U * (dy.double().abs() * top).sum(0), "dweight")
+    _near(db, dy.double().sum(0), long * U * dy.double().abs().sum(0), "dbias")
+    # in place of either, from rows further apart, and again
+    for place in ("dy", "x"):
+        one, other = _rows_apart(dy, 8), _rows_apart(x, 24)
+        into = one if place == "dy" else other
+        got = binding.layer_norm_backward(one, other, w, mean, rstd, out=(into, torch.empty_like(dw), torch.empty_like(db)))
+        assert torch.equal(into, dx) and torch.equal(got[1], dw) and torch.equal(got[2], db)
+    only = binding.layer_norm_backward(dy, x, w, mean, rstd, out=(None, torch.empty_like(dw), None))
+    assert torch.equal(only[1], dw)
+
+
+def test_gradients_over_a_hundred_thousand_rows():
+    """dweight in full where a group's column sums run over hundreds of rows."""
+    m, n = 120_001, 2048
+    x, w, _ = _rows(5, m, n, torch.bfloat16)
+    dy = torch.empty_like(x).normal_(generator=torch.Generator(device="cuda").manual_seed(6))
+    _, mean, rstd = binding.layer_norm(x, w, None, EPS)
+    dx, dw, db = binding.layer_norm_backward(dy, x, w, mean, rstd)
+    want = torch.zeros((4, n), dtype=torch.float64, device="cuda")
+    for lo in range(0, m, 20_000):
+        at = slice(lo, lo + 20_000)
+        xd, dd, rd = x[at].double(), dy[at].double(), rstd[at].double()[:, None]
+        xh = (xd - mean[at].double()[:, None]) * rd
+        gd = dd * w.double()
+        top = ((xd.abs() + mean[at].double().abs()[:, None]) * rd).amax(1, keepdim=True) + 1
+        _near(dx[at], rd * (gd - gd.mean(1, keepdim=True) - xh * (gd * xh).mean(1, keepdim=True)),
+              256 * U * rd * gd.abs().amax(1, keepdim=True) * top * top, "dx")
+        want += torch.stack([(dd * xh).sum(0), (dd.abs() * top).sum(0), dd.sum(0), dd.abs().sum(0)])
+    _near(dw, want[0], m / 148.0 * U * want[1], "dweight")
+    _near(db, want[2], m / 148.0 * U * want[3], "dbias")

@@ -1127,7 +1127,6 @@ backward_kernel(const Bwd p)
 #pragma unroll
         for (int e = 0; e < E; ++e) dw[i][e] = db[i][e] = 0.0f;
     }
-    const float inv_n = 1.0f / (float)n;
     float next_mean[R], next_rstd[R];           // of the rows behind the current ones: not waited for
     auto statistics = [&](int r) {
 #pragma unroll
@@ -1225,7 +1224,7 @@ backward_kernel(const Bwd p)
         } else {
             __syncwarp();
         }
-        v *= inv_n;
+        v = __fdiv_rn(v, (float)n);
 #pragma unroll
         for (int k = 0; k < R; ++k) {
             s1[k] = __shfl_sync(0xFFFFFFFFu, v, 2 * k * kSpan);

@@ -289,3 +289,17 @@ def test_gradients_over_a_hundred_thousand_rows():
         want += torch.stack([(dd * xh).sum(0), (dd.abs() * top).sum(0), dd.sum(0), dd.abs().sum(0)])
     _near(dw, want[0], m / 148.0 * U * want[1], "dweight")
     _near(db, want[2], m / 148.0 * U * want[3], "dbias")
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [40, 328, 392, 656, 1003, 2624, 16404])
+def test_gradients_that_cancel(n, dtype):
+    """Equal values of dy behind constant rows: the mean of g is each of them (a quotient, not a product with a rounded inverse), and
+    dx is exactly zero."""
+    m = 300
+    x = torch.randint(1, 200, (m, 1), generator=torch.Generator().manual_seed(n)).to(dtype).cuda()
+    dy = torch.flip(x, [0]).expand(m, n).contiguous()
+    mean, rstd = x[:, 0].float(), torch.full((m,), 300.0, device="cuda")
+    for rows in (x.expand(m, n).contiguous(), _rows_apart(x.expand(m, n), 1)):
+        dx, dw, db = binding.layer_norm_backward(dy, rows, None, mean, rstd)
+        assert not bool(dx.any()) and not bool(dw.any()) and torch.equal(db, dy.double().sum(0).float())

@@ -129,29 +129,35 @@ template <class T, int E> struct Piece {
     // From here on the values are converted again instead of being kept as floats, twice the registers of 16-bit ones.
     __device__ __forceinline__ void again() { asm volatile("" : "+r"(raw.x), "+r"(raw.y), "+r"(raw.z), "+r"(raw.w)); }
 };
-// The piece of columns c .. c + E - 1 of a row of n, of which some may lie outside it: zeros, or with NEAREST the row's first or
-// last value (for x in the backward pass: zero less a large mean, times rstd, may be infinite, and a zero gradient times that
-// NaN).
-template <bool NEAREST = false, class T, int E> __device__ __forceinline__ void load_at(Piece<T, E> &v, const T *row, int c, int n)
+// The piece of columns c .. c + E - 1 of a row of n, of which some may lie outside it (zeros).
+template <class T, int E> __device__ __forceinline__ void load_at(Piece<T, E> &v, const T *row, int c, int n)
 {
     if (c >= 0 && c + E <= n) {
         v.load(row + c);
     } else {
-        auto bits = [&](int at) -> uint32_t {
-            if constexpr (sizeof(T) == 4) return __float_as_uint((float)row[at]);
-            else return reinterpret_cast<const uint16_t *>(row)[at];
-        };
-        const uint32_t beside = NEAREST ? bits(c < 0 ? 0 : n - 1) : 0u;
         uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            uint32_t one = beside;
-            if (c + e >= 0 && c + e < n) one = bits(c + e);
-            if constexpr (sizeof(T) == 4) w[e] = one;
-            else w[e / 2] |= one << (16 * (e & 1));
-        }
+        for (int e = 0; e < E; ++e)
+            if (c + e >= 0 && c + e < n) {
+                if constexpr (sizeof(T) == 4) w[e] = __float_as_uint((float)row[c + e]);
+                else w[e / 2] |= (uint32_t)reinterpret_cast<const uint16_t *>(row)[c + e] << (16 * (e & 1));
+            }
         v.raw = make_uint4(w[0], w[1], w[2], w[3]);
     }
+}
+// What of it lies outside the row takes the first value that does not.
+template <class T, int E> __device__ __forceinline__ void fill_outside(Piece<T, E> &v, int c, int n)
+{
+    constexpr int kBits = 8 * (int)sizeof(T), kEach = 32 / kBits;
+    constexpr uint32_t mask = sizeof(T) == 4 ? 0xFFFFFFFFu : 0xFFFFu;
+    uint32_t w[4] = {v.raw.x, v.raw.y, v.raw.z, v.raw.w}, first = 0u;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (e == (c < 0 ? -c : 0)) first = (w[e / kEach] >> (kBits * (e % kEach))) & mask;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (c + e < 0 || c + e >= n) w[e / kEach] = (w[e / kEach] & ~(mask << (kBits * (e % kEach)))) | first << (kBits * (e % kEach));
+    v.raw = make_uint4(w[0], w[1], w[2], w[3]);
 }
 template <class T, int E> __device__ __forceinline__ void store_at(const Piece<T, E> &v, T *row, int c, int n)
 {
@@ -1168,7 +1174,7 @@ backward_kernel(const Bwd p)
             if (r < m && in_row(i)) {
                 const T *xr = x + r * p.x_pitch, *dr = dy + r * p.dy_pitch;
                 if constexpr (kShift) {
-                    load_at<true>(next_x[i], xr, c0 + i * hop, n);
+                    load_at(next_x[i], xr, c0 + i * hop, n);
                     load_at(next_d[i], dr, c0 + i * hop, n);
                 } else {
                     next_x[i].load(xr + c0 + i * hop);
@@ -1215,6 +1221,14 @@ backward_kernel(const Bwd p)
             for (int i = 0; i < V; ++i) { vx[0][i] = next_x[RING ? 0 : i]; vd[0][i] = next_d[RING ? 0 : i]; }
             load(after);
         }
+        // Columns beside the row have a zero gradient and, as they were loaded, zero as x.  Where a large mean makes their xh infinite
+        // the product of both would be NaN: such a row's take one of its values.
+        if constexpr (kShift)
+            if (!(fabsf(mean[0] * rstd[0]) <= 3.402823466e38f)) {
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (in_row(i)) fill_outside(vx[0][i], c0 + i * hop, n);
+            }
 #pragma unroll
         for (int k = 0; k < R; ++k) {
             Some t1 = all<Some>(0.0f), t2 = t1;

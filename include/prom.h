@@ -289,7 +289,8 @@ prom_status prom_layer_norm_i8(const void *x_dev, prom_type type, int64_t m, int
  *   dweight_dev, dbias_dev  [n] of param_type, overwritten; either may be NULL.  With m == 0 they are set to zero
  *   workspace_dev           16-byte aligned, prom_layer_norm_backward_workspace_bytes(m, n) bytes
  *                           (PROM_ERR_WORKSPACE if smaller); not read when dweight_dev and dbias_dev are NULL
- * Two launches.  Limits and errors as for prom_layer_norm; a copy that does not land within 0.1 s sets PROM_ERR_TIMEOUT
+ * Two launches; one without dweight_dev and dbias_dev; three for rows that registers do not hold (more than 32 KB of whole
+ * 16-byte pieces, or else more than 8192 values).  Limits and errors as for prom_layer_norm; a copy that does not land within 0.1 s sets PROM_ERR_TIMEOUT
  * in prom_last_device_status. */
 size_t prom_layer_norm_backward_workspace_bytes(int64_t m, int n);
 prom_status prom_layer_norm_backward(const void *dy_dev, const void *x_dev, prom_type type, int64_t m, int n,
@@ -327,8 +328,9 @@ typedef struct {
  *   workspace_dev             16-byte aligned, prom_pw_proj_adapters_workspace_bytes(batch, rows_per_sample, rank) bytes,
  *                not read without adapters.  Calls that may overlap need workspaces of their own
  * cin a multiple of 16, cout a multiple of 8, both up to 4096 (PROM_ERR_UNSUPPORTED, PROM_ERR_SHAPE).  The values of an
- * adapter should be finite: a value of B that is not counts as zero and sets PROM_ERR_BAD_WEIGHT in the device status
- * word, one of A shows in the rows of its own samples only.  Weight codes that are not valid surface as
+ * adapter should be finite: a value of B that is not counts as zero, so that y does not show it, and sets
+ * PROM_ERR_BAD_WEIGHT in the device status word, which a caller who serves adapters from elsewhere asks for; one of A
+ * shows in the rows of its own samples only.  Weight codes that are not valid surface as
  * PROM_ERR_BAD_WEIGHT.  Asynchronous on the stream (at most two launches); batch == 0 is a no-op.
  * Errors: PROM_ERR_NULL, PROM_ERR_SHAPE, PROM_ERR_ALIGN, PROM_ERR_RANGE (a type), PROM_ERR_WORKSPACE,
  * PROM_ERR_UNSUPPORTED, PROM_ERR_CUDA; a wait that runs out sets PROM_ERR_TIMEOUT in prom_last_device_status. */

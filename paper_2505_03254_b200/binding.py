@@ -299,7 +299,7 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opt
                eps: float = 1e-5, out=None, stream=None):
     """prom_layer_norm: x [..., n] float32, bfloat16 or float16 on the device (a matrix may have any row pitch)
     -> (y like x, mean, rstd float32, one value a row); `out` may carry the three tensors, y being x itself or the
-    last two None."""
+    last two None.  Autograd does not see the call: gradients come from layer_norm_backward."""
     if out is None:
         m = x.numel() // max(1, x.shape[-1])
         out = (_empty(x.shape, x.dtype, x.device, stream), _empty((m,), torch.float32, x.device, stream),

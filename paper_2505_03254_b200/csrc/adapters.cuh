@@ -307,8 +307,8 @@ proj_rows_kernel(const Params p)
 
 // ---- many rows: inner products ----------------------------------------------------------------------------------
 // Rows in tiles of 256.  A block sorts the tile's rows by their adapter (a row's place is the number of smaller keys), so
-// that any order of requests costs what runs of requests cost: an item is up to 32 rows of one adapter, and the items go
-// round the blocks of a tile.  K comes in stages of 256 (128 from 48 ranks on) by asynchronous copies of 16 bytes (a bulk copy
+// that rows of one adapter need not stand side by side: an item is up to 32 of the tile's rows of one adapter, and the items go
+// round the blocks of a tile.  What counts is the adapters in a tile, here and in the projection behind.  K comes in stages of 256 (128 from 48 ranks on) by asynchronous copies of 16 bytes (a bulk copy
 // per row and rank took twice as long: they are a few hundred bytes each); each of the eight warps multiplies an eighth of
 // them with the warp-level 16-bit MMA, rows as A (int8 values are exact in both 16-bit types) and the adapter as B, and the
 // warps' sums are added at the end.  A thread's 4 KS bytes of a row and 8 KS of the adapter are neighbouring values of k,
@@ -601,13 +601,15 @@ inner_tiles_kernel(const Params p)
 // operand layout on their way into shared memory (four pairs of warps take the stages in turn), so a stage takes 4 KB of
 // weights from L2 instead of 16 (a pair's SM would need 64 bytes a clock of both operands at the MMAs' rate, of the 58 that L2
 // gives it; this way it is 40).
-// 8192 rows 4096 -> 4096 with adapters of rank 64 take 142 us (161 in long runs, under the power cap), of which the inner
-// products in front take 29; without adapters 98 (2.8 POPS of 4.56).  Bound by the stages' rate, 0.4 us each where their MMAs take 0.3: narrower tiles with two accumulators of
+// 8192 rows 4096 -> 4096 with adapters of rank 64 take 148 us (170 in long runs, under the power cap), of which the inner
+// products in front take 29; without adapters 98 (2.8 POPS of 4.56).  Bound by the stages' rate, 0.4 us each where their MMAs
+// take 0.3; which part of a stage holds it there has not been measured by itself.  Narrower tiles with two accumulators of
 // each kind take longer (160 outputs 201 us, 128 outputs 223, when 256 took 154), and twice as many fillers on half as
-// many epilogue warps gain 2 % there and lose 10 % at 1024 -> 4096.
+// many epilogue warps gain 2 % there, so that the expansion is not all of it, and lose 10 % at 1024 -> 4096.
 // Behind the chunks of K come those of the adapters: for each adapter of the tile the rows' inner products (zero for rows of
 // other adapters), as sums of 16-bit values (three, or two float16 ones for 16-bit outputs) side by side along K, against B
-// repeated as often.
+// repeated as often.  An adapter costs the tile that many stages however few of its rows have it: 512 rows 4096 -> 4096 of rank
+// 16 take 33 us with two adapters and 40 with eight, of rank 64 50 and 74.
 constexpr int kFillGroups = 4, kGroupWarps = 2, kFillWarps = kFillGroups * kGroupWarps;
 constexpr int kEpiGroups = 4, kEpiWarps = 4 * kEpiGroups;
 constexpr int kFill0 = 2, kEpi0 = kFill0 + kFillWarps;

@@ -2371,7 +2371,7 @@ static prom_status launch_backward(Bwd &p, int pieces, const DeviceInfo &d, int 
     size_t smem = p.part ? (size_t)p.groups * 2 * p.n_pad * 4 : 0;
     constexpr int kRoom = 10240;        // static shared memory and what the system keeps
     if (RING) {
-        // rows in flight: as many as fit, but a whole number of steps
+        // rows in flight: as many as fit (a kernel that takes two at a time goes round an odd number too)
         const size_t stage = (size_t)2 * p.n * sizeof(T) * p.groups, room = (size_t)d.smem_optin - kRoom;
         p.stages = (int)(room / stage < (size_t)kMaxStages ? room / stage : (size_t)kMaxStages);
         if (p.stages > p.group) p.stages = p.group;

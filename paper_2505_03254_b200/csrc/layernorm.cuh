@@ -4,8 +4,9 @@
 //     g = dy w,  xh = (x - mean) rstd,  dx = rstd (g - sum(g) / n - xh sum(g xh) / n),  dw = sum_r dy xh,  db = sum_r dy
 //     gamma = max |y|,  scale = 127 / max(gamma, 1e-5),  q = clip(round(y scale), -128, 127)      (as in actquant.cuh)
 // What all of them cannot do without is their bytes: x once (and dy), y, codes or dx once.  At 16384 x 4096 bf16 the forward
-// pass takes 53.6 us (5.0 TB/s, 77 % of the measured copy bandwidth), the backward pass 76.5 to 80.5 (5.0 TB/s); 8192 x 4096 bf16 to
-// codes takes 42.1 us, there bound by its instructions (26 a value, half of them in 64 bits or for the exact quotient).
+// pass takes 53.9 us (5.0 TB/s, 76 % of the measured copy bandwidth), the backward pass 81.5 (4.9 TB/s; 76 in a replayed graph);
+// 8192 x 4096 bf16 to codes takes 42.4 us, there bound by its issue slots: 26 instructions a value, of which the 64-bit sums
+// take a share, and the affine step with its parameters, worked out once for the maximum and once for the codes.
 //
 // Many rows, forward: a warp per row, in registers or in shared memory, the parameters in shared memory.  Otherwise, and in
 // the backward pass, threads come in groups that share a row, a 16-byte piece (8 or 4 columns) each, as many groups as fill
@@ -486,7 +487,7 @@ template <class T> __device__ __forceinline__ int offset_of(const void *p) { ret
 
 // ---- forward: groups, for rows that start anywhere ------------------------------------------------------
 // V pieces a thread, two rows at a time and the next two on their way.  (576 threads are two groups for rows of 4096 and
-// some values: 8192 x 4269 bf16 70 us, 100 with 512.)
+// some values: 8192 x 4269 bf16 69.5 us, 100 with 512.)
 constexpr int kGroupThreads = 576;
 template <class T, int V, bool CODES>
 __global__ void __launch_bounds__(kGroupThreads, 1)
@@ -652,7 +653,7 @@ forward_groups_kernel(const Fwd p)
 }
 
 // ---- forward: a warp per short row ----------------------------------------------------------------------------
-// V pieces a lane, in registers, and with up to two the next row's too (25088 x 192 float32 9.8 us, 11.3 without; 16384 x 1024
+// V pieces a lane, in registers, and with up to two the next row's too (25088 x 192 float32 9.7 us, 11.3 without; 16384 x 1024
 // float16, where four run out of registers, 16.6, 14.2 without); the parameters in shared memory as in the next kernel.  (A bulk
 // copy of a row of a kilobyte costs more than its loads: 25088 x 192 float32, 14.3 us through shared memory.)
 template <class T, int V, bool CODES>
@@ -766,9 +767,9 @@ forward_short_kernel(const Fwd p)
 // ---- forward: a warp per row ------------------------------------------------------------------------------
 // For many rows of whole pieces.  No exchange between warps, and what belongs to a row worked out once for all of it.  A bulk
 // copy brings the row into shared memory, where the warp passes over it three times (four for codes): in registers the
-// longer rows leave none for the arithmetic (16 pieces a lane with the next row's copy beside all of it: 62 us against 53.8,
+// longer rows leave none for the arithmetic (16 pieces a lane with the next row's copy beside all of it: 62 us against 53.9,
 // in spilled registers).  As many warps as there is room for rows; while one waits for its row the
-// others work, and the row behind comes to L2 meanwhile (8192 x 4096 bf16 31.1 us, 33.9 without; to codes 42.3, 45.7).
+// others work, and the row behind comes to L2 meanwhile (8192 x 4096 bf16 30.8 us, 33.9 without; to codes 42.4, 45.7).
 template <class T, bool CODES>
 __global__ void __launch_bounds__(1024, 1)
 forward_warps_kernel(const Fwd p)
@@ -1338,7 +1339,7 @@ backward_kernel(const Bwd p)
     }
 }
 
-// Rows of any length: dx by a block per row, and the column sums of a slice of rows by a block per 256 columns.
+// Rows of any length: dx by a block per row, behind the column sums of a slice of rows by a block per 256 columns.
 template <class T>
 __global__ void __launch_bounds__(1024)
 backward_long_kernel(const Bwd p)
@@ -1361,8 +1362,8 @@ backward_long_kernel(const Bwd p)
         dx[c] = from_float<T>(rstd * (to_float(dy[c]) * p.w.at(c, 1.0f) - c1 - (to_float(x[c]) - mean) * rstd * c2));
 }
 
-// Launched behind backward_long_kernel without overlap: with dx == dy the column sums would read what that one wrote, so it
-// goes first (see the host code).
+// The column sums of such rows, launched in front of backward_long_kernel, which may write dx in the place of dy or x: that one
+// waits for this one's end.
 template <class T>
 __global__ void __launch_bounds__(256)
 column_sums_kernel(const Bwd p, long long rows_per_block)
